@@ -1,6 +1,7 @@
 /*
  * fq.h -- C ABI of the fused outlier-aware W4A16 decode matmul for MI355X
- * (gfx950).
+ * (gfx950), and of the operators around it in a decoder layer: the paged KV
+ * cache, attention over it and the gated residual norms (last part).
  *
  * The operation (FlashQuant, arXiv 2608.15531, eq. 1 with eq. 3):
  *
@@ -446,6 +447,200 @@ fq_status fq_w4a16_matmul(const fq_problem* pr, const uint16_t* X, const uint32_
 fq_status fq_debug_decode_tile_coo(const fq_tilecoo_dev* tc, int32_t K, int32_t N,
                                    int32_t* k_out, int32_t* n_out, uint16_t* v_out,
                                    void* stream);
+
+/* ------------------------------------------------------------------------
+ * Operators around the matmuls in a decoder layer.  They follow the
+ * conventions above: all checks on the host before anything is launched, work
+ * only enqueued on the caller's stream, nothing allocated.
+ * --------------------------------------------------------------------- */
+
+/*
+ * A paged KV cache.  Its pages hold page_size tokens each; token t of a page and
+ * KV head h has one row of K and one of V, of head_dim channels:
+ *   FQ_KV_BF16  bf16 bits.
+ *   FQ_KV_INT8  one code byte a channel.
+ *   FQ_KV_INT4  one code nibble a channel, channel 2i in the low half of byte i.
+ * A row of codes c has a scale s and a zero-point z of its own and stands for
+ * s (c - z).  s and z are the two bf16 of one 4-byte word (s in the low half) of
+ * k_meta or v_meta.  bf16 for s, since it has the range of the activations;
+ * integers up to 255 are exact in it.
+ *   k, v          device pointers, 16-byte aligned.  Row (page, head, t) starts at
+ *                 byte page * page_stride + head * head_stride + t * token_stride;
+ *                 the strides are not negative and multiples of 16, so [page][head][t]
+ *                 and [page][t][head] orders and pools with K beside V all fit.
+ *   k_meta,       device pointers to the words, 16-byte aligned; unused (NULL) with
+ *   v_meta        FQ_KV_BF16.  Word (page, head, t) lies at page * meta_page_stride +
+ *                 head * meta_head_stride + t (in words; multiples of 4).
+ *   n_pages       1 .. 2^31 - 1.
+ *   page_size     a multiple of 16, up to 65536 (FQ_ERR_UNSUPPORTED otherwise): the
+ *                 kernels take 16 tokens of one page at a time.
+ *   n_kv_heads    1 .. 65535.
+ *   head_dim      64 or 128 (FQ_ERR_UNSUPPORTED otherwise).
+ */
+enum { FQ_KV_BF16 = 0, FQ_KV_INT8 = 1, FQ_KV_INT4 = 2 };
+typedef struct {
+  void* k;
+  void* v;
+  void* k_meta;
+  void* v_meta;
+  int64_t page_stride, head_stride, token_stride;    /* bytes */
+  int64_t meta_page_stride, meta_head_stride;        /* words */
+  int64_t n_pages;
+  int32_t page_size;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t kind;
+} fq_kv_cache;
+
+/*
+ * fq_kv_cache_write -- stores new K and V rows, quantising them.
+ *   K, V       device bf16 [n_tokens][n_kv_heads][head_dim]; token and head strides in
+ *              elements, multiples of 8, and 16-byte aligned pointers, so they may be
+ *              columns of the qkv matmul's output.
+ *   slots      device int64 [n_tokens]: page * page_size + place in the page.  A token
+ *              whose slot lies outside [0, n_pages * page_size) is not stored.  Slots
+ *              must differ (otherwise which token is kept is unspecified).
+ * A row x of b bits (top = 2^b - 1), in exact arithmetic on the stored s:
+ *     hi = max(max x, 0), lo = min(min x, 0), span = hi - lo (in fp32)
+ *     s = the smallest bf16 >= span / top (1 if span is 0)
+ *     z = clamp(round(-lo / s), 0, top)
+ *     c = clamp(round(x / s) + z, 0, top)           (ties to even)
+ * A row with an infinity or a NaN, or whose span passes the largest fp32, gets s = NaN
+ * and reads back as NaN.  n_tokens may be 0.
+ * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE, FQ_ERR_UNSUPPORTED, FQ_ERR_ALIGN, FQ_ERR_HIP.
+ */
+fq_status fq_kv_cache_write(const fq_kv_cache* cache, const uint16_t* K, const uint16_t* V,
+                            int64_t k_token_stride, int64_t k_head_stride,
+                            int64_t v_token_stride, int64_t v_head_stride, const int64_t* slots,
+                            int64_t n_tokens, void* stream);
+
+/*
+ * fq_kv_cache_read -- the rows of given slots, as the values they stand for.
+ *   slots      device int64 [n_tokens], in any order, with repeats; a slot outside
+ *              [0, n_pages * page_size) gives rows of zeros.
+ *   K, V       device outputs [n_tokens][n_kv_heads][head_dim], contiguous, 16-byte
+ *              aligned; dtype FQ_Y_BF16 (rounded to nearest even once) or FQ_Y_F32 (exact).
+ * Errors: as fq_kv_cache_write.
+ */
+fq_status fq_kv_cache_read(const fq_kv_cache* cache, const int64_t* slots, int64_t n_tokens,
+                           void* K, void* V, int32_t dtype, void* stream);
+
+/*
+ * Attention of the last tokens of each sequence over a paged cache that already
+ * holds them (write first, then attend).
+ *   n_seqs      sequences, >= 1.  Sequence b has the tokens cu_q[b] .. cu_q[b+1] - 1 of Q
+ *               and kv_lens[b] tokens in the cache, these included; token j of the
+ *               sequence lies in page block_table[b][j / page_size].
+ *   total_q     tokens of Q, >= 0.
+ *   n_heads     query heads, a multiple of the cache's n_kv_heads: query head i reads KV
+ *               head i / (n_heads / n_kv_heads).
+ *   max_q,      upper bounds of the new tokens and of kv_lens over the sequences (>= 1);
+ *   max_kv      the grid and the split of the keys follow from them, not the result.
+ *               Tokens beyond max_q of a sequence are not computed and keys beyond
+ *               max_kv are not seen.
+ *   window      0: every token sees the keys up to its own.  W > 0: only the last W of
+ *               them (its own included) and the first `sinks` keys of the sequence.
+ *   sinks       >= 0; without a window it changes nothing.
+ *   scale       factor of q.k, finite.
+ *   strides     of Q and O, in elements, multiples of 8; block_table rows have
+ *               table_cols entries, table_stride apart.
+ * The new token i of a sequence stands at position p = kv_lens - q_len + i and sees key j
+ * iff j <= p and (window == 0 or j > p - window or j < sinks).  With p < 0 it sees none:
+ * its output row is 0 and its lse -infinity.  So it is too where every score is -infinity.
+ * A key that a token does not see cannot change its row, whatever the cache holds there
+ * (infinities and NaN too).
+ */
+typedef struct {
+  int32_t n_seqs;
+  int32_t n_heads;
+  int32_t max_q;
+  int32_t max_kv;
+  int32_t window;
+  int32_t sinks;
+  int64_t total_q;
+  int64_t q_token_stride, q_head_stride;
+  int64_t o_token_stride, o_head_stride;
+  int64_t table_stride;
+  int32_t table_cols;
+  float scale;
+} fq_attention;
+
+/*
+ * fq_paged_attention_workspace_bytes -- the workspace of fq_paged_attention: the
+ * same kind of workspace as the matmuls' (fq_workspace_bytes: counters that are zero
+ * between calls, then scratch), so that one buffer may serve both in turn.
+ */
+fq_status fq_paged_attention_workspace_bytes(const fq_attention* a, const fq_kv_cache* cache,
+                                             size_t* bytes);
+
+/*
+ * fq_paged_attention_launch -- the launch that a call makes (nothing is launched):
+ *   out[0] FQ_ATTN_* kernel          out[1] rows (token, query head) of a workgroup
+ *   out[2] blocks of rows per (sequence, KV head)   out[3] ranges the keys are split into
+ *   out[4] keys of a range           out[5] workgroups
+ *   out[6] LDS bytes per workgroup   out[7] workspace bytes beyond the counters, in KiB
+ * FQ_ATTN_ROWS: every wave reads its own keys straight into the matrix operands.
+ */
+enum { FQ_ATTN_ROWS = 0 };
+fq_status fq_paged_attention_launch(const fq_attention* a, const fq_kv_cache* cache,
+                                    int32_t out[8]);
+
+/*
+ * fq_paged_attention -- softmax(scale q K^T) V of the keys each token sees.
+ *   Q            device bf16, row (t, head) at t * q_token_stride + head * q_head_stride.
+ *   cu_q         device int32 [n_seqs + 1], from 0, not decreasing, at most total_q.
+ *   kv_lens      device int32 [n_seqs], >= 0.
+ *   block_table  device int32; entries of pages that a token sees lie in [0, n_pages).
+ *   O            device bf16, rounded to nearest even once; rows as Q.
+ *   lse          device fp32 [total_q][n_heads]: ln of the sum of exp(scale q.k); NULL: not
+ *                written.
+ * Q, O 16-byte aligned.  Scores, softmax statistics and sums are held in fp32; the softmax
+ * weights (times the scale of V's row) are rounded to bf16 as the matrix operand.  The sums of the
+ * ranges are added in their order, so equal calls give equal bits.  Index contents out of
+ * range cannot make the kernel read or write out of bounds but give unspecified values.
+ * Rows of O that belong to no sequence are not written.
+ * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE, FQ_ERR_UNSUPPORTED, FQ_ERR_ALIGN, FQ_ERR_WORKSPACE,
+ * FQ_ERR_HIP.
+ */
+fq_status fq_paged_attention(const fq_attention* a, const uint16_t* Q, const fq_kv_cache* cache,
+                             const int32_t* cu_q, const int32_t* kv_lens,
+                             const int32_t* block_table, uint16_t* O, float* lse,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * fq_gated_residual_norm -- the norm after a block, its gate, the residual sum and the
+ * norm before the next block, in one pass over the rows:
+ *     u = x / rms(x) * post_weight            (u = x without post_weight)
+ *     r = residual_scale * residual + gate * u
+ *     h = r / rms(r) * pre_weight             rms(v) = sqrt(mean(v^2) + eps)
+ * in fp32 from the inputs on; r and h are rounded once each (h comes from the r before
+ * its rounding).
+ *   rows, cols      cols 1 .. 32768 (FQ_ERR_UNSUPPORTED above), rows >= 0.
+ *   x               device [rows][cols], x_dtype FQ_Y_BF16 or FQ_Y_F32.
+ *   residual        device, residual_dtype; NULL: r = gate * u.
+ *   post_weight     device bf16 [cols] or NULL.
+ *   gate            device bf16, row i at i * gate_stride (0: one gate for all rows); NULL: 1.
+ *   pre_weight      device bf16 [cols]; needed with h.
+ *   residual_out    device, residual_dtype: r; may be residual itself; NULL: not written.
+ *   h               device bf16; NULL: not computed.
+ * One of residual_out and h at least.  Strides are of rows, in elements; columns are
+ * contiguous.  Any alignment of the element's own size is accepted; rows that are all
+ * 16-byte aligned (with cols a multiple of 8) are read in wide loads.
+ * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE, FQ_ERR_UNSUPPORTED, FQ_ERR_ALIGN, FQ_ERR_HIP.
+ */
+typedef struct {
+  int64_t rows;
+  int32_t cols;
+  int32_t x_dtype;
+  int32_t residual_dtype;
+  float eps;
+  float residual_scale;
+  int64_t x_stride, residual_stride, gate_stride, residual_out_stride, h_stride;
+} fq_norm;
+fq_status fq_gated_residual_norm(const fq_norm* n, const void* x, const void* residual,
+                                 const uint16_t* post_weight, const uint16_t* gate,
+                                 const uint16_t* pre_weight, void* residual_out, uint16_t* h,
+                                 void* stream);
 
 /* Human-readable name of a status code (static storage). */
 const char* fq_status_string(fq_status s);

@@ -1,4 +1,5 @@
-"""Python binding of libfq (fused outlier-aware W4A16 decode matmul, MI355X).
+"""Python binding of libfq (fused outlier-aware W4A16 decode matmul, MI355X, and
+the operators around it in a decoder layer: paged KV cache, attention, norms).
 
 Argument marshalling only: every step of the computation runs in the HIP
 kernels of libfq.so, behind the C ABI declared in include/fq.h.  PyTorch
@@ -11,6 +12,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import math
 import os
 import threading
 from dataclasses import dataclass
@@ -44,6 +46,12 @@ FQ_STRIP_32 = 16
 FQ_STRIP_64 = 32
 FQ_SPARSE_WAVES = 64
 FQ_DENSE_VALU = 128
+FQ_KV_BF16 = 0
+FQ_KV_INT8 = 1
+FQ_KV_INT4 = 2
+_KV_KINDS = {"bf16": FQ_KV_BF16, "int8": FQ_KV_INT8, "int4": FQ_KV_INT4}
+FQ_ATTN_ROWS = 0
+_ATTN_KERNELS = {FQ_ATTN_ROWS: "rows"}
 
 
 class FqError(RuntimeError):
@@ -83,6 +91,32 @@ class fq_problem(C.Structure):
                 ("flags", C.c_int32)]
 
 
+class fq_kv_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_meta", C.c_void_p),
+                ("v_meta", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("token_stride", C.c_int64), ("meta_page_stride", C.c_int64),
+                ("meta_head_stride", C.c_int64), ("n_pages", C.c_int64),
+                ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("kind", C.c_int32)]
+
+
+class fq_attention(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_heads", C.c_int32), ("max_q", C.c_int32),
+                ("max_kv", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32),
+                ("total_q", C.c_int64), ("q_token_stride", C.c_int64),
+                ("q_head_stride", C.c_int64), ("o_token_stride", C.c_int64),
+                ("o_head_stride", C.c_int64), ("table_stride", C.c_int64),
+                ("table_cols", C.c_int32), ("scale", C.c_float)]
+
+
+class fq_norm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int32), ("x_dtype", C.c_int32),
+                ("residual_dtype", C.c_int32), ("eps", C.c_float), ("residual_scale", C.c_float),
+                ("x_stride", C.c_int64), ("residual_stride", C.c_int64),
+                ("gate_stride", C.c_int64), ("residual_out_stride", C.c_int64),
+                ("h_stride", C.c_int64)]
+
+
 _lib = None
 _lock = threading.Lock()
 
@@ -119,6 +153,16 @@ _SIGS = {
     "fq_fill_padding_slots": ([C.c_int32, C.c_int32, _P, C.c_int32,
                                C.POINTER(fq_tilecoo_params), C.c_int64, _P, _P, _P, _P, _P,
                                C.POINTER(C.c_int64)], C.c_int),
+    "fq_kv_cache_write": ([C.POINTER(fq_kv_cache), _P, _P, C.c_int64, C.c_int64, C.c_int64,
+                           C.c_int64, _P, C.c_int64, _P], C.c_int),
+    "fq_kv_cache_read": ([C.POINTER(fq_kv_cache), _P, C.c_int64, _P, _P, C.c_int32, _P], C.c_int),
+    "fq_paged_attention_workspace_bytes": ([C.POINTER(fq_attention), C.POINTER(fq_kv_cache),
+                                            C.POINTER(C.c_size_t)], C.c_int),
+    "fq_paged_attention_launch": ([C.POINTER(fq_attention), C.POINTER(fq_kv_cache),
+                                   C.POINTER(C.c_int32)], C.c_int),
+    "fq_paged_attention": ([C.POINTER(fq_attention), _P, C.POINTER(fq_kv_cache), _P, _P, _P, _P,
+                            _P, _P, C.c_size_t, _P], C.c_int),
+    "fq_gated_residual_norm": ([C.POINTER(fq_norm), _P, _P, _P, _P, _P, _P, _P, _P], C.c_int),
 }
 EXPORTS = tuple(_SIGS)
 
@@ -585,6 +629,300 @@ def fq_workspace_bytes_unfused(M: int, K: int, N: int, y_dtype=FQ_Y_BF16, split_
     _check(lib.fq_workspace_bytes_unfused(C.byref(pr), C.byref(need)),
            "fq_workspace_bytes_unfused")
     return need.value
+
+
+# ------------------------------------------- the rest of a decoder layer --
+
+def _check_rows(t, dtype, shape, name):
+    """A CUDA tensor whose last dimension is contiguous; the others may have any stride."""
+    if not isinstance(t, _torch().Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} "
+                         f"{tuple(t.shape)}")
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    if 1 in shape[:-1]:   # torch keeps any number as the stride of a dimension of one
+        st = tuple(0 if n == 1 else s for n, s in zip(shape, st))
+    return st
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, not on {device}")
+
+
+class KVCache:
+    """A paged KV cache over device tensors (fq.h, fq_kv_cache).
+
+    k, v: [n_pages][n_kv_heads][page_size][row], bf16 with kind "bf16" (row =
+    head_dim), uint8 with "int8" (row = head_dim) and "int4" (row = head_dim / 2);
+    k_meta, v_meta: bf16 [n_pages][n_kv_heads][page_size][2], scale and zero-point.
+    The tensors may be views with other strides (k and v with the same ones), such as
+    pools ordered [n_pages][page_size][n_kv_heads][row] seen through transpose(1, 2)."""
+
+    def __init__(self, k, v, k_meta=None, v_meta=None, kind: str = "bf16"):
+        torch = _torch()
+        if kind not in _KV_KINDS:
+            raise ValueError(f"kind: one of {sorted(_KV_KINDS)}, got {kind!r}")
+        dtype = torch.bfloat16 if kind == "bf16" else torch.uint8
+        if not isinstance(k, torch.Tensor) or k.dim() != 4:
+            raise ValueError("k: expected [n_pages][n_kv_heads][page_size][row]")
+        st = _check_rows(k, dtype, k.shape, "k")
+        if _check_rows(v, dtype, k.shape, "v") != st:
+            raise ValueError("k and v must have the same strides")
+        P, H, T, row = k.shape
+        size = k.element_size()
+        mst = (0, 0, 1)
+        if kind == "bf16":
+            if k_meta is not None or v_meta is not None:
+                raise ValueError("a bf16 cache has no k_meta and v_meta")
+        else:
+            if k_meta is None or v_meta is None:
+                raise ValueError(f"a cache of kind {kind} needs k_meta and v_meta")
+            m = _check_rows(k_meta, torch.bfloat16, (P, H, T, 2), "k_meta")
+            if _check_rows(v_meta, torch.bfloat16, (P, H, T, 2), "v_meta") != m:
+                raise ValueError("k_meta and v_meta must have the same strides")
+            if (T > 1 and m[2] != 2) or m[0] % 2 or m[1] % 2:
+                raise ValueError("k_meta, v_meta: the tokens of a page must be contiguous")
+            mst = (m[0] // 2, m[1] // 2, 1)
+        _same_device(k.device, v=v, k_meta=k_meta, v_meta=v_meta)
+        self.k, self.v, self.k_meta, self.v_meta, self.kind = k, v, k_meta, v_meta, kind
+        self.device = k.device
+        self.n_pages, self.n_kv_heads, self.page_size = P, H, T
+        self.head_dim = 2 * row if kind == "int4" else row
+        self._struct = fq_kv_cache(
+            k.data_ptr(), v.data_ptr(), None if k_meta is None else k_meta.data_ptr(),
+            None if v_meta is None else v_meta.data_ptr(), st[0] * size, st[1] * size,
+            st[2] * size, mst[0], mst[1], P, T, H, self.head_dim, _KV_KINDS[kind])
+        self._ref = C.byref(self._struct)
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int,
+              kind: str = "bf16", device="cuda") -> "KVCache":
+        """A cache whose pages hold nothing yet."""
+        torch = _torch()
+        if kind not in _KV_KINDS:
+            raise ValueError(f"kind: one of {sorted(_KV_KINDS)}, got {kind!r}")
+        row = head_dim // 2 if kind == "int4" else head_dim
+        dtype = torch.bfloat16 if kind == "bf16" else torch.uint8
+        k, v = (torch.empty((n_pages, n_kv_heads, page_size, row), dtype=dtype, device=device)
+                for _ in range(2))
+        if kind == "bf16":
+            return cls(k, v, kind=kind)
+        km, vm = (torch.empty((n_pages, n_kv_heads, page_size, 2), dtype=torch.bfloat16,
+                              device=device) for _ in range(2))
+        return cls(k, v, km, vm, kind=kind)
+
+    def struct(self) -> fq_kv_cache:
+        return self._struct
+
+    @property
+    def nbytes(self) -> int:
+        return sum(t.numel() * t.element_size()
+                   for t in (self.k, self.v, self.k_meta, self.v_meta) if t is not None)
+
+
+class PagedBatch:
+    """The sequences of one step: cu_q int32 [n_seqs + 1] (first new token of each),
+    kv_lens int32 [n_seqs] (tokens in the cache, the new ones included), block_table
+    int32 [n_seqs][pages], and upper bounds max_q and max_kv of the new tokens and of
+    kv_lens.  Made once for all layers of a step; the tensors' contents may change
+    between calls within the bounds (as under graph replay)."""
+
+    def __init__(self, cu_q, kv_lens, block_table, max_q: int, max_kv: int):
+        torch = _torch()
+        if not isinstance(kv_lens, torch.Tensor) or kv_lens.dim() != 1:
+            raise ValueError("kv_lens: expected [n_seqs]")
+        n = kv_lens.shape[0]
+        _check_tensor(kv_lens, torch.int32, (n,), "kv_lens")
+        _check_tensor(cu_q, torch.int32, (n + 1,), "cu_q")
+        if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
+            raise ValueError("block_table: expected [n_seqs][pages]")
+        st = _check_rows(block_table, torch.int32, (n, block_table.shape[1]), "block_table")
+        _same_device(cu_q.device, kv_lens=kv_lens, block_table=block_table)
+        self.cu_q, self.kv_lens, self.block_table = cu_q, kv_lens, block_table
+        self.n_seqs, self.max_q, self.max_kv = n, int(max_q), int(max_kv)
+        self.table_stride = st[0]
+        self.device = cu_q.device
+        self._pointers = (cu_q.data_ptr(), kv_lens.data_ptr(), block_table.data_ptr())
+
+
+def fq_kv_cache_write(cache: KVCache, k, v, slots, stream=None) -> None:
+    """Store the rows k, v (bf16 [n_tokens][n_kv_heads][head_dim], any token and head
+    stride) at `slots` (int64 [n_tokens]: page * page_size + place; a token whose slot is
+    out of range, such as -1, is not stored), quantised as the cache's kind asks."""
+    torch = _torch()
+    shape = (slots.shape[0], cache.n_kv_heads, cache.head_dim)
+    ks = _check_rows(k, torch.bfloat16, shape, "k")
+    vs = _check_rows(v, torch.bfloat16, shape, "v")
+    _check_tensor(slots, torch.int64, shape[:1], "slots")
+    _same_device(cache.device, k=k, v=v, slots=slots)
+    _check(load().fq_kv_cache_write(cache._ref, k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0],
+                                    vs[1], slots.data_ptr(), shape[0],
+                                    _stream_handle(stream, cache.device)), "fq_kv_cache_write")
+
+
+def fq_kv_cache_read(cache: KVCache, slots, k=None, v=None, dtype="bf16", stream=None):
+    """The rows at `slots` (int64 [n_tokens]; out of range: zeros) as the values they
+    stand for; returns K, V of [n_tokens][n_kv_heads][head_dim], bf16 or fp32 ("f32")."""
+    torch = _torch()
+    f32 = dtype in ("f32", "fp32", torch.float32)
+    if not isinstance(slots, torch.Tensor) or slots.dim() != 1:
+        raise ValueError("slots: expected int64 [n_tokens]")
+    _check_tensor(slots, torch.int64, slots.shape, "slots")
+    shape = (slots.shape[0], cache.n_kv_heads, cache.head_dim)
+    dt = torch.float32 if f32 else torch.bfloat16
+    with _on_stream(stream):
+        if k is None:
+            k = torch.empty(shape, dtype=dt, device=cache.device)
+        else:
+            _check_tensor(k, dt, shape, "k")
+        if v is None:
+            v = torch.empty(shape, dtype=dt, device=cache.device)
+        else:
+            _check_tensor(v, dt, shape, "v")
+    _same_device(cache.device, k=k, v=v, slots=slots)
+    _check(load().fq_kv_cache_read(cache._ref, slots.data_ptr(), shape[0], k.data_ptr(),
+                                   v.data_ptr(), FQ_Y_F32 if f32 else FQ_Y_BF16,
+                                   _stream_handle(stream, cache.device)), "fq_kv_cache_read")
+    return k, v
+
+
+def _attention(n_heads, q_strides, o_strides, total_q, cache, batch, scale, window, sinks):
+    return fq_attention(batch.n_seqs, n_heads, batch.max_q, batch.max_kv, window, sinks, total_q,
+                        q_strides[0], q_strides[1], o_strides[0], o_strides[1],
+                        batch.table_stride, batch.block_table.shape[1],
+                        1.0 / math.sqrt(cache.head_dim) if scale is None else scale)
+
+
+def fq_paged_attention(q, cache: KVCache, batch: PagedBatch, scale: float | None = None,
+                       window: int = 0, sinks: int = 0, out=None, return_lse: bool = False,
+                       stream=None, ws=None):
+    """Attention of the new tokens q (bf16 [total_q][n_heads][head_dim], any token and
+    head stride) over the cache, which holds their K and V already.  scale: default
+    1 / sqrt(head_dim).  window W > 0: a token sees the last W keys up to its own and the
+    first `sinks` keys.  Returns out (bf16, like q), and with return_lse also the ln of
+    the softmax sums, fp32 [total_q][n_heads].  A token that sees no key gets zeros and
+    -infinity; rows of q that belong to no sequence are left as they are in `out`
+    (unspecified in a new one)."""
+    torch = _torch()
+    lib = load()
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q: expected [total_q][n_heads][head_dim]")
+    shape = q.shape
+    device = cache.device
+    qs = _check_rows(q, torch.bfloat16, (shape[0], shape[1], cache.head_dim), "q")
+    _same_device(device, q=q, cu_q=batch.cu_q)
+    lse = None
+    with _on_stream(stream):
+        if out is None:
+            out = torch.empty(shape, dtype=torch.bfloat16, device=device)
+        else:
+            _same_device(device, out=out)
+        if return_lse:
+            lse = torch.empty(shape[:2], dtype=torch.float32, device=device)
+    a = _attention(shape[1], qs, _check_rows(out, torch.bfloat16, shape, "out"), shape[0], cache,
+                   batch, scale, window, sinks)
+    ref = C.byref(a)
+    cu, lens, table = batch._pointers
+    sh = _stream_handle(stream, device)
+
+    def call(w):
+        return lib.fq_paged_attention(ref, q.data_ptr(), cache._ref, cu, lens, table,
+                                      out.data_ptr(), None if lse is None else lse.data_ptr(),
+                                      None if w is None else w.data_ptr(),
+                                      0 if w is None else w.numel(), sh)
+
+    status = call(ws if ws is not None else _workspaces.get((device.index, sh)))
+    if status == _FQ_ERR_WORKSPACE and ws is None:
+        # checked before anything is enqueued: none is kept yet, or too small a one
+        need = C.c_size_t(0)
+        _check(lib.fq_paged_attention_workspace_bytes(ref, cache._ref, C.byref(need)),
+               "fq_paged_attention_workspace_bytes")
+        with _on_stream(stream):
+            status = call(workspace(need.value, device, sh))
+    _check(status, "fq_paged_attention")
+    return (out, lse) if return_lse else out
+
+
+def fq_paged_attention_workspace_bytes(n_heads: int, total_q: int, cache: KVCache,
+                                       batch: PagedBatch, window: int = 0, sinks: int = 0) -> int:
+    a = _attention(n_heads, (0, 0), (0, 0), total_q, cache, batch, None, window, sinks)
+    need = C.c_size_t(0)
+    _check(load().fq_paged_attention_workspace_bytes(C.byref(a), cache._ref, C.byref(need)),
+           "fq_paged_attention_workspace_bytes")
+    return need.value
+
+
+def fq_paged_attention_launch(n_heads: int, total_q: int, cache: KVCache, batch: PagedBatch,
+                              window: int = 0, sinks: int = 0) -> dict:
+    """The kernel and grid of a call (nothing is launched)."""
+    a = _attention(n_heads, (0, 0), (0, 0), total_q, cache, batch, None, window, sinks)
+    out = (C.c_int32 * 8)()
+    _check(load().fq_paged_attention_launch(C.byref(a), cache._ref, out),
+           "fq_paged_attention_launch")
+    return {"kernel": _ATTN_KERNELS[out[0]], "rows": out[1], "row_blocks": out[2],
+            "split": out[3], "split_keys": out[4], "workgroups": out[5], "lds_bytes": out[6],
+            "partial_kib": out[7]}
+
+
+def _dtype_code(dtype, name):
+    torch = _torch()
+    if dtype == torch.bfloat16:
+        return FQ_Y_BF16
+    if dtype == torch.float32:
+        return FQ_Y_F32
+    raise ValueError(f"{name}: expected bfloat16 or float32, got {dtype}")
+
+
+def fq_gated_residual_norm(x, residual=None, pre_weight=None, post_weight=None, gate=None,
+                           residual_scale: float = 1.0, eps: float = 1e-5, residual_out=None,
+                           h=None, stream=None):
+    """u = RMSNorm(x) post_weight (x itself without post_weight), r = residual_scale
+    residual + gate u, h = RMSNorm(r) pre_weight, each rounded once; returns (r, h).
+
+    x [rows][cols] bf16 or fp32; residual the same shape, bf16 or fp32 (None: r = gate u,
+    of x's type); gate bf16 [cols] or [rows][cols] (None: 1); weights bf16 [cols].
+    Without pre_weight only r is computed and h is None.  residual_out may be residual.
+    Rows may have any stride; columns are contiguous."""
+    torch = _torch()
+    lib = load()
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("x: expected [rows][cols]")
+    shape = x.shape
+    M, H = shape
+    xs = _check_rows(x, x.dtype, shape, "x")
+    rt = x.dtype if residual is None else residual.dtype
+    n = fq_norm(M, H, _dtype_code(x.dtype, "x"), _dtype_code(rt, "residual"), eps, residual_scale,
+                xs[0], 0, 0, 0, 0)
+    if residual is not None:
+        n.residual_stride = _check_rows(residual, rt, shape, "residual")[0]
+    if gate is not None:
+        if gate.dim() == 1:
+            _check_rows(gate, torch.bfloat16, (H,), "gate")
+        else:
+            n.gate_stride = _check_rows(gate, torch.bfloat16, shape, "gate")[0]
+    for w, name in ((post_weight, "post_weight"), (pre_weight, "pre_weight")):
+        if w is not None:
+            _check_rows(w, torch.bfloat16, (H,), name)
+    with _on_stream(stream):
+        if residual_out is None:
+            residual_out = torch.empty(shape, dtype=rt, device=x.device)
+        if h is None and pre_weight is not None:
+            h = torch.empty(shape, dtype=torch.bfloat16, device=x.device)
+    n.residual_out_stride = _check_rows(residual_out, rt, shape, "residual_out")[0]
+    if h is not None:
+        n.h_stride = _check_rows(h, torch.bfloat16, shape, "h")[0]
+    _same_device(x.device, residual=residual, pre_weight=pre_weight, post_weight=post_weight,
+                 gate=gate, residual_out=residual_out, h=h)
+    ptr = [None if t is None else t.data_ptr()
+           for t in (residual, post_weight, gate, pre_weight, residual_out, h)]
+    _check(lib.fq_gated_residual_norm(C.byref(n), x.data_ptr(), *ptr,
+                                      _stream_handle(stream, x.device)), "fq_gated_residual_norm")
+    return residual_out, h
 
 
 # ---------------------------------------------------- numpy -> device --

@@ -27,8 +27,10 @@ GEMM_LIB_PATH = os.path.join(HERE, "libfqgemm.so")
 GEMM_SOURCES = ["gemm_ref.cpp"]
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
-HOST_SOURCES = ["capi.cpp", "tilecoo.cpp", "quant.cpp"]
+HOST_SOURCES = ["capi.cpp", "layer.cpp", "tilecoo.cpp", "quant.cpp"]
 HIP_SOURCES = ["kernels.hip", "rows.hip"]
+# kernels that the instrumented build has without stamps, from the same objects
+PLAIN_HIP_SOURCES = ["kvcache.hip", "attention.hip", "norm.hip"]
 
 # Packed-fp32 VALU forms are kept out of every HIP object.  MFMA results stay
 # in ordinary VGPRs (the accumulation registers would need a copy-out per
@@ -73,7 +75,7 @@ def build(verbose: bool = False) -> str:
         obj = os.path.join(BUILD_DIR, src + ".o")
         jobs.append(["g++", *HOST_FLAGS, "-D__HIP_PLATFORM_AMD__", "-isystem",
                      os.path.join(ROCM, "include"), *incs, "-c", os.path.join(CSRC, src), "-o", obj])
-    for src in HIP_SOURCES + PROBE_SOURCES:
+    for src in HIP_SOURCES + PLAIN_HIP_SOURCES + PROBE_SOURCES:
         obj = os.path.join(BUILD_DIR, src + ".o")
         jobs.append([_hipcc(), *HIP_FLAGS, *incs, "-c", os.path.join(CSRC, src), "-o", obj])
     stamp_objs = []
@@ -88,7 +90,7 @@ def build(verbose: bool = False) -> str:
     probe_objs = [o for o in objs if os.path.basename(o)[:-2] in PROBE_SOURCES]
     gemm_objs = [o for o in objs if os.path.basename(o)[:-2] in GEMM_SOURCES]
     lib_objs = [o for o in objs if o not in probe_objs and o not in gemm_objs]
-    host_objs = [o for o in lib_objs if os.path.basename(o)[:-2] in HOST_SOURCES]
+    host_objs = [o for o in lib_objs if os.path.basename(o)[:-2] in HOST_SOURCES + PLAIN_HIP_SOURCES]
     for path, ob in ((LIB_PATH, lib_objs), (PROBE_LIB_PATH, probe_objs),
                      (STAMPS_LIB_PATH, host_objs + stamp_objs)):
         tmp = path + ".tmp"

@@ -1,0 +1,640 @@
+// Attention of new tokens over a paged KV cache (fq_paged_attention).
+//
+// Rows.  The query heads that share a KV head see the same keys, so a "row" is one
+// (token, query head) of a sequence and a KV head, and the G = n_heads / n_kv_heads
+// heads of a token are G neighbouring rows.  A workgroup takes a block of 16 rows of
+// one (sequence, KV head) and one range of the keys; its four waves take tiles of 32
+// keys in turn and join their results at the end.
+//
+// Products.  Both run on v_mfma_f32_16x16x32_bf16, as S^T = K Q^T and O^T = V^T P^T, so
+// that a lane holds everything of its row (lane & 15): with S^T as the result its 8
+// scores of a tile belong to the keys 4 q .. 4 q + 3 and 16 + 4 q .. (q = lane >> 4),
+// and those are, packed to bf16, just the 8 k-slots that the lane feeds to the second
+// product.  Running maximum, sum, rescaling and output scale need no exchange but the
+// maximum over the four lanes of a row.  The order of the k-slots is free as long as
+// both operands agree: K rows come from memory 16 bytes a lane, and V, of which an
+// operand needs 8 keys of one channel, is read as 8 keys x 8 channels a lane and put
+// together by byte permutes, two keys to a register.  Nothing goes through LDS.
+//
+// Quantised caches.  A code c becomes a bf16 exactly (4 bits: 128 + c by one and-or,
+// 8 bits: through fp32), and the affine map is applied to the sums:
+//     q . k = s_k (sum q c - z_k sum q),   sum p v = sum p' c - sum p' z_v,
+//     p' = bf16(p s_v).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <climits>
+
+#include "device.hpp"
+#include "internal.hpp"
+#include "layer.hpp"
+
+namespace fqk {
+
+namespace {
+
+using fqi::kKvBlock;
+using fqi::kKvTile;
+
+struct AttnArgs {
+  const uint16_t* Q;
+  const char* k;
+  const char* v;
+  const uint32_t* k_meta;
+  const uint32_t* v_meta;
+  const int32_t* cu_q;
+  const int32_t* kv_lens;
+  const int32_t* table;
+  uint16_t* O;
+  float* lse;
+  float* partials;
+  uint32_t* counters;
+  int64_t page_stride, head_stride, meta_page_stride, meta_head_stride, table_stride;
+  int64_t q_token, q_head, o_token, o_head, total_q;
+  uint32_t token_stride;   // bytes
+  uint32_t page_blocks;    // kKvBlock-token blocks in a page
+  uint32_t n_pages;
+  int group;               // query heads per KV head
+  int n_heads;
+  int max_q, max_kv, window, sinks;
+  int row_blocks, split, split_tiles, part_rows;
+  float scale_log2;        // scale * log2(e): the softmax runs in powers of two
+};
+
+typedef __bf16 bf16x2v __attribute__((__vector_size__(4)));
+
+__device__ __forceinline__ uint32_t pk_bf16(float lo, float hi) {
+  const bf16x2v r = {static_cast<__bf16>(lo), static_cast<__bf16>(hi)};
+  return __builtin_bit_cast(uint32_t, r);
+}
+
+__device__ __forceinline__ f32x4_t mfma16(bf16x8_t a, bf16x8_t b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// Maximum and sum over the four lanes of a row (lanes l, l ^ 16, l ^ 32, l ^ 48).
+__device__ __forceinline__ float row_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float row_add(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
+// Channels of the lane's 8 k-slots in product step `st` of S^T: the first of them.
+// They follow from the 16 (or 8) bytes of a K row that a lane loads at once.
+template <int KIND, int D>
+__device__ __forceinline__ int q_channel(int st, int q) {
+  if constexpr (KIND == FQ_KV_BF16) return st * 32 + q * 8;
+  else if constexpr (KIND == FQ_KV_INT8) return (st >> 1) * 64 + q * 16 + (st & 1) * 8;
+  else return q * (D / 4) + st * 8;
+}
+
+// One K row's share of a lane: the codes or bf16 of all its k-slots.
+template <int KIND, int D>
+struct KRow {
+  static constexpr int W = KIND == FQ_KV_BF16 ? D / 8 : KIND == FQ_KV_INT8 ? D / 16 : D / 32;
+  uint32_t w[W];
+  __device__ __forceinline__ void load(const char* row, int q) {
+    if constexpr (W >= 4) {
+#pragma unroll
+      for (int i = 0; i < W / 4; ++i) {
+        const uint4 x = *reinterpret_cast<const uint4*>(row + i * 64 + q * 16);
+        w[4 * i] = x.x;
+        w[4 * i + 1] = x.y;
+        w[4 * i + 2] = x.z;
+        w[4 * i + 3] = x.w;
+      }
+    } else {
+      const uint2 x = *reinterpret_cast<const uint2*>(row + q * 8);
+      w[0] = x.x;
+      w[1] = x.y;
+    }
+  }
+  __device__ __forceinline__ bf16x8_t operand(int st) const {
+    u32x4_t r;
+    if constexpr (KIND == FQ_KV_BF16) {
+      r = u32x4_t{w[4 * st], w[4 * st + 1], w[4 * st + 2], w[4 * st + 3]};
+    } else if constexpr (KIND == FQ_KV_INT8) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t c = w[2 * st + i / 2] >> (16 * (i & 1));
+        r[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, float((c >> 8) & 255u)),
+                                     __builtin_bit_cast(uint32_t, float(c & 255u)), 0x07060302u);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = and_or(w[st] >> (4 * i), 0x000F000Fu, 0x43004300u);
+    }
+    return __builtin_bit_cast(bf16x8_t, r);
+  }
+};
+
+// The offset that operand() adds to the codes.
+template <int KIND>
+constexpr float kKvOffset = KIND == FQ_KV_INT4 ? kCodeOffset : 0.f;
+
+// Eight V rows' share of a lane: D / 16 channels from (lane & 15) * D / 16 on.
+template <int KIND, int D>
+struct VRows {
+  static constexpr int C = D / 16;   // channels a lane = 16-channel blocks of O^T
+  static constexpr int BYTES = KIND == FQ_KV_BF16 ? 2 * C : KIND == FQ_KV_INT8 ? C : C / 2;
+  static constexpr int W = (BYTES + 3) / 4;
+  uint32_t w[8][W];
+  __device__ __forceinline__ void load(int j, const char* row, int c16) {
+    const char* p = row + c16 * BYTES;
+    if constexpr (BYTES == 16) {
+      const uint4 x = *reinterpret_cast<const uint4*>(p);
+      w[j][0] = x.x;
+      w[j][1] = x.y;
+      w[j][2] = x.z;
+      w[j][3] = x.w;
+    } else if constexpr (BYTES == 8) {
+      const uint2 x = *reinterpret_cast<const uint2*>(p);
+      w[j][0] = x.x;
+      w[j][1] = x.y;
+    } else if constexpr (BYTES == 4) {
+      w[j][0] = *reinterpret_cast<const uint32_t*>(p);
+    } else {
+      w[j][0] = *reinterpret_cast<const uint16_t*>(p);
+    }
+  }
+  // The A operand of channel block c: two keys to a register.
+  __device__ __forceinline__ bf16x8_t operand(int c) const {
+    u32x4_t r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t* a = w[2 * i];
+      const uint32_t* b = w[2 * i + 1];
+      if constexpr (KIND == FQ_KV_BF16) {
+        r[i] = __builtin_amdgcn_perm(b[c / 2], a[c / 2], (c & 1) ? 0x07060302u : 0x05040100u);
+      } else if constexpr (KIND == FQ_KV_INT8) {
+        const uint32_t x = (a[c / 4] >> (8 * (c & 3))) & 255u, y = (b[c / 4] >> (8 * (c & 3))) & 255u;
+        r[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, float(y)), __builtin_bit_cast(uint32_t, float(x)),
+                                     0x07060302u);
+      } else {
+        const uint32_t t = __builtin_amdgcn_perm(b[0], a[0], c < 4 ? 0x05040100u : 0x07060302u);
+        r[i] = and_or(t >> (4 * (c & 3)), 0x000F000Fu, 0x43004300u);
+      }
+    }
+    return __builtin_bit_cast(bf16x8_t, r);
+  }
+};
+
+// Which tiles a block of rows at positions [p_lo, p_hi] sees: with a window, the tiles of
+// the first keys and those of the window, numbered one after the other.
+struct TileRange {
+  int first;   // tiles of the first keys
+  int skip;    // tiles between those and the window
+  int n;
+  __device__ __forceinline__ int tile(int i) const { return i < first ? i : i + skip; }
+};
+
+__device__ __forceinline__ TileRange tile_range(int p_lo, int p_hi, int window, int sinks) {
+  TileRange r;
+  const int end = p_hi < 0 ? 0 : p_hi / kKvTile + 1;   // p_hi is the last key seen
+  r.first = 0;
+  r.skip = 0;
+  if (window > 0 && p_lo >= window) {
+    const int lo = (p_lo - window + 1) / kKvTile;
+    r.first = min(lo, (min(sinks, p_lo + 1) + kKvTile - 1) / kKvTile);
+    r.skip = lo - r.first;
+  }
+  r.n = max(0, end - r.skip);
+  return r;
+}
+
+// Infinities and NaN of bf16 rows that some row of the block sees and another does not:
+// 0 x infinity would put a NaN into the latter.  The finite rest goes through the product
+// as always; what is not finite is counted by products with indicators of its three kinds
+// and the mask, and added where the count is not zero.
+template <int D>
+__device__ __forceinline__ bool has_nonfinite(const VRows<FQ_KV_BF16, D>& v) {
+  bool any = false;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+#pragma unroll
+    for (int i = 0; i < VRows<FQ_KV_BF16, D>::W; ++i) {
+      const uint32_t x = v.w[j][i];
+      any |= (x & 0x7F80u) == 0x7F80u || (x & 0x7F800000u) == 0x7F800000u;
+    }
+  return __any(any);
+}
+
+// Splits an operand of V: returns its finite numbers, and adds to `acc` what the others
+// (kind 0 +infinity, 1 -infinity, 2 NaN) give the rows that see them (`seen`: 1 or 0 in
+// the place of the weights).
+__device__ __forceinline__ bf16x8_t take_nonfinite(bf16x8_t operand, u32x4_t seen, f32x4_t& acc) {
+  u32x4_t r = __builtin_bit_cast(u32x4_t, operand);
+#pragma unroll 1
+  for (int kind = 0; kind < 3; ++kind) {
+    const uint32_t lo = kind == 0 ? 0x7F80u : kind == 1 ? 0xFF80u : 0x7F81u;
+    const uint32_t hi = kind == 2 ? 0x7FFFu : lo, sign = kind == 2 ? 0x7FFFu : 0xFFFFu;
+    u32x4_t ind;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t a = r[i] & sign, b = (r[i] >> 16) & sign;
+      ind[i] = (a >= lo && a <= hi ? 0x3F80u : 0u) | (b >= lo && b <= hi ? 0x3F800000u : 0u);
+    }
+    const f32x4_t count = mfma16(__builtin_bit_cast(bf16x8_t, ind), __builtin_bit_cast(bf16x8_t, seen),
+                                 f32x4_t{0.f, 0.f, 0.f, 0.f});
+    const float what = __builtin_bit_cast(float, kind == 0 ? 0x7F800000u : kind == 1 ? 0xFF800000u : 0x7FC00000u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (count[i] > 0.f) acc[i] += what;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((r[i] & 0x7F80u) == 0x7F80u) r[i] &= 0xFFFF0000u;
+    if ((r[i] & 0x7F800000u) == 0x7F800000u) r[i] &= 0x0000FFFFu;
+  }
+  return __builtin_bit_cast(bf16x8_t, r);
+}
+
+constexpr int kWaves = 4;
+constexpr float kNegInf = -__builtin_inff();
+
+// LDS: the waves' sums [kWaves][16][D + 4], then their maxima and row sums.
+template <int D>
+constexpr size_t kAttnLds = (size_t(kWaves) * 16 * (D + 4) + 2 * kWaves * 16) * 4;
+
+template <int KIND, int D>
+__global__ void __launch_bounds__(64 * kWaves) attn_rows_kernel(AttnArgs a) {
+  constexpr int STEPS = D / 32, CB = D / 16;
+  extern __shared__ float lds[];
+  __shared__ uint32_t last_flag;
+  float* l_acc = lds;
+  float* l_max = lds + kWaves * 16 * (D + 4);
+  float* l_sum = l_max + kWaves * 16;
+  const int tid = int(threadIdx.x), lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r16 = lane & 15, q = lane >> 4;
+
+  const int rb = int(blockIdx.x) % a.row_blocks, sp = int(blockIdx.x) / a.row_blocks;
+  const int head = int(blockIdx.y), seq = int(blockIdx.z);
+  const int64_t t0 = min(max(int64_t(a.cu_q[seq]), int64_t(0)), a.total_q);
+  const int64_t t1 = min(max(int64_t(a.cu_q[seq + 1]), t0), a.total_q);
+  const int q_all = int(t1 - t0);               // before the bound: positions count from the end
+  const int q_len = min(q_all, a.max_q);
+  const int kv_len = max(a.kv_lens[seq], 0);
+  const int64_t n_rows = int64_t(q_len) * a.group;
+  const int64_t row0 = int64_t(rb) * 16;
+  if (row0 >= n_rows) return;
+  const int rows = int(min(n_rows - row0, int64_t(16)));
+  const int tok_lo = int(row0 / a.group), tok_hi = int((row0 + rows - 1) / a.group);
+  const int p0 = kv_len - q_all;                // position of the first new token
+  const int kv_seen = min(kv_len, a.max_kv);
+  const int p_lo = min(p0 + tok_lo, kv_seen - 1), p_hi = min(p0 + tok_hi, kv_seen - 1);
+  const TileRange tr = tile_range(p_lo, p_hi, a.window, a.sinks);
+  const int n_parts = min(max(1, (tr.n + a.split_tiles - 1) / a.split_tiles), a.split);
+  if (sp >= n_parts) return;
+  const int i_lo = sp * a.split_tiles, i_hi = min(i_lo + a.split_tiles, tr.n);
+
+  // this lane's row
+  const bool row_in = r16 < rows;
+  const int row_tok = int((row0 + min(r16, rows - 1)) / a.group);
+  const int row_g = int(row0 + min(r16, rows - 1) - int64_t(row_tok) * a.group);
+  const int pos = row_in ? min(p0 + row_tok, kv_seen - 1) : -1;
+  const int win_lo = a.window > 0 ? (p0 + row_tok) - a.window + 1 : INT_MIN;   // first key of the window
+  const int q_head = head * a.group + row_g;
+  const uint16_t* qp = a.Q + (t0 + row_tok) * a.q_token + q_head * a.q_head;
+  bf16x8_t qv[STEPS];
+  float q_sum = 0.f;
+#pragma unroll
+  for (int st = 0; st < STEPS; ++st) {
+    uint4 w{0, 0, 0, 0};
+    if (row_in) w = *reinterpret_cast<const uint4*>(qp + q_channel<KIND, D>(st, q));
+    if constexpr (KIND != FQ_KV_BF16) {
+      const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        q_sum += bf16_bits_to_f32(ws[i]) + __builtin_bit_cast(float, ws[i] & 0xFFFF0000u);
+    }
+    if constexpr (KIND == FQ_KV_INT4) w = permute_chunk(w);
+    qv[st] = __builtin_bit_cast(bf16x8_t, w);
+  }
+  if constexpr (KIND != FQ_KV_BF16) q_sum = row_add(q_sum);
+
+  f32x4_t acc[CB];
+#pragma unroll
+  for (int c = 0; c < CB; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float m = kNegInf, l = 0.f, corr = 0.f;
+
+  const int32_t* table = a.table + seq * a.table_stride;
+  const char* kh = a.k + head * a.head_stride;
+  const char* vh = a.v + head * a.head_stride;
+  const uint32_t* kmh = KIND == FQ_KV_BF16 ? nullptr : a.k_meta + head * a.meta_head_stride;
+  const uint32_t* vmh = KIND == FQ_KV_BF16 ? nullptr : a.v_meta + head * a.meta_head_stride;
+
+  for (int i = i_lo + wave; i < i_hi; i += kWaves) {
+    const int key0 = tr.tile(i) * kKvTile;
+    KRow<KIND, D> kr[2];
+    VRows<KIND, D> vr;
+    uint4 km[2], vm[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      // a block past the last key is masked: any page in range will do
+      const int key = key0 + h * kKvBlock;
+      const uint32_t blk = uint32_t(key < kv_seen ? key : key0) / kKvBlock;
+      const uint32_t col = blk / a.page_blocks;
+      const uint32_t page = min(uint32_t(table[col]), a.n_pages - 1);
+      const uint32_t tok = (blk - col * a.page_blocks) * kKvBlock;
+      const char* kb = kh + page * a.page_stride + tok * int64_t(a.token_stride);
+      const char* vb = vh + page * a.page_stride + tok * int64_t(a.token_stride);
+      kr[h].load(kb + uint32_t(r16) * a.token_stride, q);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) vr.load(4 * h + j, vb + uint32_t(4 * q + j) * a.token_stride, r16);
+      if constexpr (KIND != FQ_KV_BF16) {
+        km[h] = *reinterpret_cast<const uint4*>(kmh + page * a.meta_page_stride + tok + 4 * q);
+        vm[h] = *reinterpret_cast<const uint4*>(vmh + page * a.meta_page_stride + tok + 4 * q);
+      }
+    }
+    // scores, in powers of two
+    float s[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      f32x4_t d{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) d = mfma16(kr[h].operand(st), qv[st], d);
+      const uint32_t kmw[4] = {km[h].x, km[h].y, km[h].z, km[h].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (KIND == FQ_KV_BF16) {
+          s[4 * h + j] = d[j] * a.scale_log2;
+        } else {
+          const float z = __builtin_bit_cast(float, kmw[j] & 0xFFFF0000u) + kKvOffset<KIND>;
+          s[4 * h + j] = fmaf(-z, q_sum, d[j]) * (bf16_bits_to_f32(kmw[j]) * a.scale_log2);
+        }
+      }
+    }
+    // the mask, where the tile is not seen whole by every row
+    const bool whole = key0 + kKvTile - 1 <= p_lo &&
+                       (a.window == 0 || key0 > p0 + tok_hi - a.window || key0 + kKvTile <= a.sinks);
+    uint32_t seen = 0xFFu;
+    if (!whole) {
+      seen = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int key = key0 + (j >> 2) * kKvBlock + 4 * q + (j & 3);
+        const bool see = key <= pos && (key >= win_lo || key < a.sinks);
+        seen |= uint32_t(see) << j;
+        s[j] = see ? s[j] : kNegInf;
+      }
+    }
+    float top = s[0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) top = fmaxf(top, s[j]);
+    top = row_max(top);
+    const float m_new = fmaxf(m, top);
+    const float base = m_new == kNegInf ? 0.f : m_new;
+    const float shrink = __builtin_amdgcn_exp2f(m - base);
+    m = m_new;
+    float p[8];
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      p[j] = __builtin_amdgcn_exp2f(s[j] - base);
+      sum += p[j];
+    }
+    l = fmaf(l, shrink, sum);
+    u32x4_t pw;
+    if constexpr (KIND == FQ_KV_BF16) {
+#pragma unroll
+      for (int i2 = 0; i2 < 4; ++i2) pw[i2] = pk_bf16(p[2 * i2], p[2 * i2 + 1]);
+    } else {
+      const uint32_t vmw[8] = {vm[0].x, vm[0].y, vm[0].z, vm[0].w, vm[1].x, vm[1].y, vm[1].z, vm[1].w};
+      corr *= shrink;
+#pragma unroll
+      for (int i2 = 0; i2 < 4; ++i2) {
+        const uint32_t m0 = vmw[2 * i2], m1 = vmw[2 * i2 + 1];
+        // a key that is not seen counts nothing, whatever its scale
+        const float a0 = (seen >> (2 * i2)) & 1u ? p[2 * i2] * bf16_bits_to_f32(m0) : 0.f;
+        const float a1 = (seen >> (2 * i2 + 1)) & 1u ? p[2 * i2 + 1] * bf16_bits_to_f32(m1) : 0.f;
+        pw[i2] = pk_bf16(a0, a1);
+        const float b0 = bf16_bits_to_f32(pw[i2]), b1 = __builtin_bit_cast(float, pw[i2] & 0xFFFF0000u);
+        const float z0 = (seen >> (2 * i2)) & 1u ? __builtin_bit_cast(float, m0 & 0xFFFF0000u) : 0.f;
+        const float z1 = (seen >> (2 * i2 + 1)) & 1u ? __builtin_bit_cast(float, m1 & 0xFFFF0000u) : 0.f;
+        corr = fmaf(b0, z0 + kKvOffset<KIND>, corr);
+        corr = fmaf(b1, z1 + kKvOffset<KIND>, corr);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < CB; ++c) acc[c] *= shrink;
+    const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, pw);
+    bool clean = true;
+    if constexpr (KIND == FQ_KV_BF16) clean = whole || !has_nonfinite<D>(vr);
+    if (clean) {
+#pragma unroll
+      for (int c = 0; c < CB; ++c) acc[c] = mfma16(vr.operand(c), pb, acc[c]);
+    } else {
+      u32x4_t sw;
+#pragma unroll
+      for (int i2 = 0; i2 < 4; ++i2)
+        sw[i2] = ((seen >> (2 * i2)) & 1u ? 0x3F80u : 0u) | ((seen >> (2 * i2 + 1)) & 1u ? 0x3F800000u : 0u);
+#pragma unroll
+      for (int c = 0; c < CB; ++c) {
+        const bf16x8_t v = take_nonfinite(vr.operand(c), sw, acc[c]);
+        acc[c] = mfma16(v, pb, acc[c]);
+      }
+    }
+  }
+
+  // join the waves: lane (r16, q) has channels (4 q + i) CB + c of row r16
+  l = row_add(l);
+  if constexpr (KIND != FQ_KV_BF16) corr = row_add(corr);
+  {
+    float* dst = l_acc + (wave * 16 + r16) * (D + 4) + 4 * q * CB;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < CB; c += 4)
+        *reinterpret_cast<f32x4_t*>(dst + i * CB + c) =
+            f32x4_t{acc[c][i] - corr, acc[c + 1][i] - corr, acc[c + 2][i] - corr, acc[c + 3][i] - corr};
+    if (q == 0) {
+      l_max[wave * 16 + r16] = m;
+      l_sum[wave * 16 + r16] = l;
+    }
+  }
+  __syncthreads();
+  // thread (row, channels ch .. ch + CB - 1)
+  const int row = tid >> 4, ch = (tid & 15) * CB;
+  float o[CB], mx = kNegInf, sum = 0.f;
+#pragma unroll
+  for (int c = 0; c < CB; ++c) o[c] = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) mx = fmaxf(mx, l_max[w * 16 + row]);
+  const float base = mx == kNegInf ? 0.f : mx;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    // (a NaN maximum cannot be: fmaxf drops it; the sum then is NaN)
+    const float f = __builtin_amdgcn_exp2f(l_max[w * 16 + row] - base);
+    sum = fmaf(f, l_sum[w * 16 + row], sum);
+    const float* src = l_acc + (w * 16 + row) * (D + 4) + ch;
+#pragma unroll
+    for (int c = 0; c < CB; ++c) o[c] = fmaf(f, src[c], o[c]);
+  }
+
+  if (n_parts > 1) {
+    // partial sums: [item][range][row][D] floats, then [item][range][row][2]
+    const int64_t item = (int64_t(seq) * gridDim.y + head) * a.row_blocks + rb;
+    const uint32_t part_words = uint32_t(a.part_rows) * (D + 4);
+    float* base_p = a.partials + item * a.split * part_words;
+    const __amdgpu_buffer_rsrc_t prs = make_rsrc(base_p, uint32_t(a.split) * part_words * 4u);
+    if (row < rows) {
+      const uint32_t at = (uint32_t(sp) * part_words + uint32_t(row) * (D + 4)) * 4u;
+#pragma unroll
+      for (int c = 0; c < CB; c += 4)
+        __builtin_amdgcn_raw_buffer_store_b128(
+            __builtin_bit_cast(u32x4_t, f32x4_t{o[c], o[c + 1], o[c + 2], o[c + 3]}), prs, int(at + (ch + c) * 4u), 0, kSc1);
+      if ((tid & 15) == 0)
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, f32x4_t{mx, sum, 0.f, 0.f}), prs,
+                                               int(at + D * 4u), 0, kSc1);
+    }
+    __builtin_amdgcn_s_waitcnt(0);   // this thread's partial stores have completed
+    __syncthreads();
+    if (tid == 0) {
+      const uint32_t old = __hip_atomic_fetch_add(a.counters + item, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      last_flag = old == uint32_t(n_parts - 1);
+    }
+    __syncthreads();
+    if (!last_flag) return;
+    if (tid == 0) __hip_atomic_store(a.counters + item, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (row >= rows) return;
+    // the last to arrive adds the ranges in their order
+    mx = kNegInf;
+    sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < CB; ++c) o[c] = 0.f;
+    for (int s2 = 0; s2 < n_parts; ++s2) {
+      const uint32_t at = (uint32_t(s2) * part_words + uint32_t(row) * (D + 4)) * 4u;
+      const f32x4_t ms = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(prs, int(at + D * 4u), 0, kSc1));
+      const float m2 = fmaxf(mx, ms[0]);
+      const float b2 = m2 == kNegInf ? 0.f : m2;
+      const float f0 = __builtin_amdgcn_exp2f(mx - b2), f1 = __builtin_amdgcn_exp2f(ms[0] - b2);
+      mx = m2;
+      sum = fmaf(sum, f0, f1 * ms[1]);
+#pragma unroll
+      for (int c = 0; c < CB; c += 4) {
+        const f32x4_t v = __builtin_bit_cast(
+            f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(prs, int(at + (ch + c) * 4u), 0, kSc1));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[c + i] = fmaf(o[c + i], f0, f1 * v[i]);
+      }
+    }
+  }
+  if (row >= rows) return;
+  const int64_t r = row0 + row;
+  const int tok = int(r / a.group);
+  const int oh = head * a.group + int(r - int64_t(tok) * a.group);
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  uint16_t* op = a.O + (t0 + tok) * a.o_token + oh * a.o_head + ch;
+  uint32_t w[CB / 2];
+#pragma unroll
+  for (int c = 0; c < CB; c += 2)
+    w[c / 2] = sum == 0.f ? 0u : pk_bf16(o[c] * inv, o[c + 1] * inv);
+  if constexpr (CB == 8) *reinterpret_cast<uint4*>(op) = uint4{w[0], w[1], w[2], w[3]};
+  else *reinterpret_cast<uint2*>(op) = uint2{w[0], w[1]};
+  if (a.lse && (tid & 15) == 0)
+    a.lse[(t0 + tok) * a.n_heads + oh] = sum == 0.f ? kNegInf : (mx + __log2f(sum)) * 0.69314718055994530942f;
+}
+
+}  // namespace
+
+}  // namespace fqk
+
+namespace fqi {
+
+namespace {
+
+constexpr int kTargetWorkgroups = 1024;   // four to a CU
+constexpr int kMinSplitTiles = 8;         // 256 keys a range: two tiles a wave
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+}  // namespace
+
+bool plan_attention(const fq_attention& a, const fq_kv_cache& c, AttnPlan* pl) {
+  const int64_t group = a.n_heads / c.n_kv_heads;
+  const int64_t row_blocks = ceil_div(a.max_q * group, 16);
+  if (row_blocks > (1 << 24) || a.n_seqs > 65535) return false;
+  pl->rows = 16;
+  pl->row_blocks = int(row_blocks);
+  const int64_t items = row_blocks * c.n_kv_heads * a.n_seqs;
+  // tiles that a block of rows can see at most
+  int64_t tiles = ceil_div(a.max_kv, kKvTile);
+  if (a.window > 0)
+    tiles = std::min<int64_t>(tiles, ceil_div(a.window + ceil_div(16, group), kKvTile) + 2 + ceil_div(a.sinks, kKvTile));
+  // enough ranges to fill the GPU, none of them short; every item has a counter
+  int64_t split = 1;
+  if (items <= kMaxStrips && items < kTargetWorkgroups)
+    split = std::max<int64_t>(1, std::min(ceil_div(kTargetWorkgroups, items), tiles / kMinSplitTiles));
+  pl->split_tiles = int(ceil_div(tiles, split));
+  pl->split = int(ceil_div(tiles, pl->split_tiles));
+  if (pl->split * row_blocks > INT32_MAX) return false;
+  pl->workgroups = items * pl->split;
+  if (pl->workgroups > INT32_MAX) return false;
+  pl->lds_bytes = c.head_dim == 64 ? fqk::kAttnLds<64> : fqk::kAttnLds<128>;
+  const int part_rows = int(std::min<int64_t>(16, a.max_q * group));
+  pl->partial_bytes = pl->split > 1 ? size_t(items) * pl->split * part_rows * (c.head_dim + 4) * 4 : 0;
+  pl->ws_bytes = kCounterRegion + pl->partial_bytes;
+  return true;
+}
+
+int launch_attention(const AttnPlan& pl, const fq_attention& a, const fq_kv_cache& c,
+                     const uint16_t* Q, const int32_t* cu_q, const int32_t* kv_lens,
+                     const int32_t* table, uint16_t* O, float* lse, void* workspace,
+                     void* stream) {
+  const int group = a.n_heads / c.n_kv_heads;
+  fqk::AttnArgs g{};
+  g.Q = Q;
+  g.k = static_cast<const char*>(c.k);
+  g.v = static_cast<const char*>(c.v);
+  g.k_meta = static_cast<const uint32_t*>(c.k_meta);
+  g.v_meta = static_cast<const uint32_t*>(c.v_meta);
+  g.cu_q = cu_q;
+  g.kv_lens = kv_lens;
+  g.table = table;
+  g.O = O;
+  g.lse = lse;
+  g.counters = static_cast<uint32_t*>(workspace);
+  g.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterRegion);
+  g.page_stride = c.page_stride;
+  g.head_stride = c.head_stride;
+  g.meta_page_stride = c.meta_page_stride;
+  g.meta_head_stride = c.meta_head_stride;
+  g.table_stride = a.table_stride;
+  g.q_token = a.q_token_stride;
+  g.q_head = a.q_head_stride;
+  g.o_token = a.o_token_stride;
+  g.o_head = a.o_head_stride;
+  g.total_q = a.total_q;
+  g.token_stride = uint32_t(c.token_stride);
+  g.page_blocks = uint32_t(c.page_size / kKvBlock);
+  g.n_pages = uint32_t(c.n_pages);
+  g.group = group;
+  g.n_heads = a.n_heads;
+  g.max_q = a.max_q;
+  g.max_kv = a.max_kv;
+  g.window = a.window;
+  g.sinks = a.sinks;
+  g.row_blocks = pl.row_blocks;
+  g.split = pl.split;
+  g.split_tiles = pl.split_tiles;
+  g.part_rows = int(std::min<int64_t>(16, int64_t(a.max_q) * group));
+  g.scale_log2 = a.scale * 1.44269504088896340736f;
+  const dim3 grid(unsigned(pl.row_blocks * pl.split), unsigned(c.n_kv_heads), unsigned(a.n_seqs));
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  auto go = [&](auto kind) {
+    if (c.head_dim == 64)
+      hipLaunchKernelGGL((fqk::attn_rows_kernel<kind.value, 64>), grid, dim3(64 * fqk::kWaves), pl.lds_bytes, s, g);
+    else
+      hipLaunchKernelGGL((fqk::attn_rows_kernel<kind.value, 128>), grid, dim3(64 * fqk::kWaves), pl.lds_bytes, s, g);
+  };
+  if (c.kind == FQ_KV_BF16) go(std::integral_constant<int, FQ_KV_BF16>{});
+  else if (c.kind == FQ_KV_INT8) go(std::integral_constant<int, FQ_KV_INT8>{});
+  else go(std::integral_constant<int, FQ_KV_INT4>{});
+  return int(hipGetLastError());
+}
+
+}  // namespace fqi
