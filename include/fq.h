@@ -535,7 +535,8 @@ fq_status fq_kv_cache_read(const fq_kv_cache* cache, const int64_t* slots, int64
  *   n_heads     query heads, a multiple of the cache's n_kv_heads: query head i reads KV
  *               head i / (n_heads / n_kv_heads).
  *   max_q,      upper bounds of the new tokens and of kv_lens over the sequences (>= 1);
- *   max_kv      the grid and the split of the keys follow from them, not the result.
+ *   max_kv      up to 2^28; the kernel, its grid and the split of the keys follow from
+ *               them, and the result only in its rounding.
  *               Tokens beyond max_q of a sequence are not computed and keys beyond
  *               max_kv are not seen.
  *   window      0: every token sees the keys up to its own.  W > 0: only the last W of
@@ -579,9 +580,10 @@ fq_status fq_paged_attention_workspace_bytes(const fq_attention* a, const fq_kv_
  *   out[2] blocks of rows per (sequence, KV head)   out[3] ranges the keys are split into
  *   out[4] keys of a range           out[5] workgroups
  *   out[6] LDS bytes per workgroup   out[7] workspace bytes beyond the counters, in KiB
- * FQ_ATTN_ROWS: every wave reads its own keys straight into the matrix operands.
+ * FQ_ATTN_ROWS, for few rows: every wave reads its own keys straight into the matrix
+ * operands.  FQ_ATTN_TILES, for many: the waves share tiles of keys through LDS.
  */
-enum { FQ_ATTN_ROWS = 0 };
+enum { FQ_ATTN_ROWS = 0, FQ_ATTN_TILES = 1 };
 fq_status fq_paged_attention_launch(const fq_attention* a, const fq_kv_cache* cache,
                                     int32_t out[8]);
 

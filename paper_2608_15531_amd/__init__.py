@@ -51,7 +51,8 @@ FQ_KV_INT8 = 1
 FQ_KV_INT4 = 2
 _KV_KINDS = {"bf16": FQ_KV_BF16, "int8": FQ_KV_INT8, "int4": FQ_KV_INT4}
 FQ_ATTN_ROWS = 0
-_ATTN_KERNELS = {FQ_ATTN_ROWS: "rows"}
+FQ_ATTN_TILES = 1
+_ATTN_KERNELS = {FQ_ATTN_ROWS: "rows", FQ_ATTN_TILES: "tiles"}
 
 
 class FqError(RuntimeError):

@@ -30,7 +30,7 @@ ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HOST_SOURCES = ["capi.cpp", "layer.cpp", "tilecoo.cpp", "quant.cpp"]
 HIP_SOURCES = ["kernels.hip", "rows.hip"]
 # kernels that the instrumented build has without stamps, from the same objects
-PLAIN_HIP_SOURCES = ["kvcache.hip", "attention.hip", "norm.hip"]
+PLAIN_HIP_SOURCES = ["kvcache.hip", "attention.hip", "attention_tiles.hip", "norm.hip"]
 
 # Packed-fp32 VALU forms are kept out of every HIP object.  MFMA results stay
 # in ordinary VGPRs (the accumulation registers would need a copy-out per

@@ -20,57 +20,13 @@
 // 8 bits: through fp32), and the affine map is applied to the sums:
 //     q . k = s_k (sum q c - z_k sum q),   sum p v = sum p' c - sum p' z_v,
 //     p' = bf16(p s_v).
-#include <hip/hip_runtime.h>
-
 #include <algorithm>
-#include <climits>
 
-#include "device.hpp"
-#include "internal.hpp"
-#include "layer.hpp"
+#include "attention.hpp"
 
 namespace fqk {
 
 namespace {
-
-using fqi::kKvBlock;
-using fqi::kKvTile;
-
-struct AttnArgs {
-  const uint16_t* Q;
-  const char* k;
-  const char* v;
-  const uint32_t* k_meta;
-  const uint32_t* v_meta;
-  const int32_t* cu_q;
-  const int32_t* kv_lens;
-  const int32_t* table;
-  uint16_t* O;
-  float* lse;
-  float* partials;
-  uint32_t* counters;
-  int64_t page_stride, head_stride, meta_page_stride, meta_head_stride, table_stride;
-  int64_t q_token, q_head, o_token, o_head, total_q;
-  uint32_t token_stride;   // bytes
-  uint32_t page_blocks;    // kKvBlock-token blocks in a page
-  uint32_t n_pages;
-  int group;               // query heads per KV head
-  int n_heads;
-  int max_q, max_kv, window, sinks;
-  int row_blocks, split, split_tiles, part_rows;
-  float scale_log2;        // scale * log2(e): the softmax runs in powers of two
-};
-
-typedef __bf16 bf16x2v __attribute__((__vector_size__(4)));
-
-__device__ __forceinline__ uint32_t pk_bf16(float lo, float hi) {
-  const bf16x2v r = {static_cast<__bf16>(lo), static_cast<__bf16>(hi)};
-  return __builtin_bit_cast(uint32_t, r);
-}
-
-__device__ __forceinline__ f32x4_t mfma16(bf16x8_t a, bf16x8_t b, f32x4_t c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
 
 // Maximum and sum over the four lanes of a row (lanes l, l ^ 16, l ^ 32, l ^ 48).
 __device__ __forceinline__ float row_max(float v) {
@@ -182,78 +138,7 @@ struct VRows {
   }
 };
 
-// Which tiles a block of rows at positions [p_lo, p_hi] sees: with a window, the tiles of
-// the first keys and those of the window, numbered one after the other.
-struct TileRange {
-  int first;   // tiles of the first keys
-  int skip;    // tiles between those and the window
-  int n;
-  __device__ __forceinline__ int tile(int i) const { return i < first ? i : i + skip; }
-};
-
-__device__ __forceinline__ TileRange tile_range(int p_lo, int p_hi, int window, int sinks) {
-  TileRange r;
-  const int end = p_hi < 0 ? 0 : p_hi / kKvTile + 1;   // p_hi is the last key seen
-  r.first = 0;
-  r.skip = 0;
-  if (window > 0 && p_lo >= window) {
-    const int lo = (p_lo - window + 1) / kKvTile;
-    r.first = min(lo, (min(sinks, p_lo + 1) + kKvTile - 1) / kKvTile);
-    r.skip = lo - r.first;
-  }
-  r.n = max(0, end - r.skip);
-  return r;
-}
-
-// Infinities and NaN of bf16 rows that some row of the block sees and another does not:
-// 0 x infinity would put a NaN into the latter.  The finite rest goes through the product
-// as always; what is not finite is counted by products with indicators of its three kinds
-// and the mask, and added where the count is not zero.
-template <int D>
-__device__ __forceinline__ bool has_nonfinite(const VRows<FQ_KV_BF16, D>& v) {
-  bool any = false;
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-#pragma unroll
-    for (int i = 0; i < VRows<FQ_KV_BF16, D>::W; ++i) {
-      const uint32_t x = v.w[j][i];
-      any |= (x & 0x7F80u) == 0x7F80u || (x & 0x7F800000u) == 0x7F800000u;
-    }
-  return __any(any);
-}
-
-// Splits an operand of V: returns its finite numbers, and adds to `acc` what the others
-// (kind 0 +infinity, 1 -infinity, 2 NaN) give the rows that see them (`seen`: 1 or 0 in
-// the place of the weights).
-__device__ __forceinline__ bf16x8_t take_nonfinite(bf16x8_t operand, u32x4_t seen, f32x4_t& acc) {
-  u32x4_t r = __builtin_bit_cast(u32x4_t, operand);
-#pragma unroll 1
-  for (int kind = 0; kind < 3; ++kind) {
-    const uint32_t lo = kind == 0 ? 0x7F80u : kind == 1 ? 0xFF80u : 0x7F81u;
-    const uint32_t hi = kind == 2 ? 0x7FFFu : lo, sign = kind == 2 ? 0x7FFFu : 0xFFFFu;
-    u32x4_t ind;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t a = r[i] & sign, b = (r[i] >> 16) & sign;
-      ind[i] = (a >= lo && a <= hi ? 0x3F80u : 0u) | (b >= lo && b <= hi ? 0x3F800000u : 0u);
-    }
-    const f32x4_t count = mfma16(__builtin_bit_cast(bf16x8_t, ind), __builtin_bit_cast(bf16x8_t, seen),
-                                 f32x4_t{0.f, 0.f, 0.f, 0.f});
-    const float what = __builtin_bit_cast(float, kind == 0 ? 0x7F800000u : kind == 1 ? 0xFF800000u : 0x7FC00000u);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (count[i] > 0.f) acc[i] += what;
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if ((r[i] & 0x7F80u) == 0x7F80u) r[i] &= 0xFFFF0000u;
-    if ((r[i] & 0x7F800000u) == 0x7F800000u) r[i] &= 0x0000FFFFu;
-  }
-  return __builtin_bit_cast(bf16x8_t, r);
-}
-
 constexpr int kWaves = 4;
-constexpr float kNegInf = -__builtin_inff();
 
 // LDS: the waves' sums [kWaves][16][D + 4], then their maxima and row sums.
 template <int D>
@@ -262,7 +147,7 @@ constexpr size_t kAttnLds = (size_t(kWaves) * 16 * (D + 4) + 2 * kWaves * 16) * 
 template <int KIND, int D>
 __global__ void __launch_bounds__(64 * kWaves) attn_rows_kernel(AttnArgs a) {
   constexpr int STEPS = D / 32, CB = D / 16;
-  extern __shared__ float lds[];
+  extern __shared__ __attribute__((aligned(16))) float lds[];
   __shared__ uint32_t last_flag;
   float* l_acc = lds;
   float* l_max = lds + kWaves * 16 * (D + 4);
@@ -271,40 +156,17 @@ __global__ void __launch_bounds__(64 * kWaves) attn_rows_kernel(AttnArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, q = lane >> 4;
 
-  const int rb = int(blockIdx.x) % a.row_blocks, sp = int(blockIdx.x) / a.row_blocks;
-  const int head = int(blockIdx.y), seq = int(blockIdx.z);
-  const int64_t t0 = min(max(int64_t(a.cu_q[seq]), int64_t(0)), a.total_q);
-  const int64_t t1 = min(max(int64_t(a.cu_q[seq + 1]), t0), a.total_q);
-  const int q_all = int(t1 - t0);               // before the bound: positions count from the end
-  const int q_len = min(q_all, a.max_q);
-  const int kv_len = max(a.kv_lens[seq], 0);
-  const int64_t n_rows = int64_t(q_len) * a.group;
-  const int64_t row0 = int64_t(rb) * 16;
-  if (row0 >= n_rows) return;
-  const int rows = int(min(n_rows - row0, int64_t(16)));
-  const int tok_lo = int(row0 / a.group), tok_hi = int((row0 + rows - 1) / a.group);
-  const int p0 = kv_len - q_all;                // position of the first new token
-  const int kv_seen = min(kv_len, a.max_kv);
-  const int p_lo = min(p0 + tok_lo, kv_seen - 1), p_hi = min(p0 + tok_hi, kv_seen - 1);
-  const TileRange tr = tile_range(p_lo, p_hi, a.window, a.sinks);
-  const int n_parts = min(max(1, (tr.n + a.split_tiles - 1) / a.split_tiles), a.split);
-  if (sp >= n_parts) return;
-  const int i_lo = sp * a.split_tiles, i_hi = min(i_lo + a.split_tiles, tr.n);
-
-  // this lane's row
-  const bool row_in = r16 < rows;
-  const int row_tok = int((row0 + min(r16, rows - 1)) / a.group);
-  const int row_g = int(row0 + min(r16, rows - 1) - int64_t(row_tok) * a.group);
-  const int pos = row_in ? min(p0 + row_tok, kv_seen - 1) : -1;
-  const int win_lo = a.window > 0 ? (p0 + row_tok) - a.window + 1 : INT_MIN;   // first key of the window
-  const int q_head = head * a.group + row_g;
-  const uint16_t* qp = a.Q + (t0 + row_tok) * a.q_token + q_head * a.q_head;
+  Item it;
+  if (!it.set<16, kKvTile>(a)) return;
+  Row mine;
+  mine.set(a, it, r16);
+  const uint16_t* qp = a.Q + (it.t0 + mine.token) * a.q_token + mine.head * a.q_head;
   bf16x8_t qv[STEPS];
   float q_sum = 0.f;
 #pragma unroll
   for (int st = 0; st < STEPS; ++st) {
     uint4 w{0, 0, 0, 0};
-    if (row_in) w = *reinterpret_cast<const uint4*>(qp + q_channel<KIND, D>(st, q));
+    if (mine.in) w = *reinterpret_cast<const uint4*>(qp + q_channel<KIND, D>(st, q));
     if constexpr (KIND != FQ_KV_BF16) {
       const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -320,15 +182,16 @@ __global__ void __launch_bounds__(64 * kWaves) attn_rows_kernel(AttnArgs a) {
 #pragma unroll
   for (int c = 0; c < CB; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   float m = kNegInf, l = 0.f, corr = 0.f;
+  bool odd = false;   // V had infinities or NaN in a tile that is not seen whole
 
-  const int32_t* table = a.table + seq * a.table_stride;
-  const char* kh = a.k + head * a.head_stride;
-  const char* vh = a.v + head * a.head_stride;
-  const uint32_t* kmh = KIND == FQ_KV_BF16 ? nullptr : a.k_meta + head * a.meta_head_stride;
-  const uint32_t* vmh = KIND == FQ_KV_BF16 ? nullptr : a.v_meta + head * a.meta_head_stride;
+  const int32_t* table = a.table + it.seq * a.table_stride;
+  const char* kh = a.k + it.head * a.head_stride;
+  const char* vh = a.v + it.head * a.head_stride;
+  const uint32_t* kmh = KIND == FQ_KV_BF16 ? nullptr : a.k_meta + it.head * a.meta_head_stride;
+  const uint32_t* vmh = KIND == FQ_KV_BF16 ? nullptr : a.v_meta + it.head * a.meta_head_stride;
 
-  for (int i = i_lo + wave; i < i_hi; i += kWaves) {
-    const int key0 = tr.tile(i) * kKvTile;
+  for (int i = it.i_lo + wave; i < it.i_hi; i += kWaves) {
+    const int key0 = it.tr.tile(i) * kKvTile;
     KRow<KIND, D> kr[2];
     VRows<KIND, D> vr;
     uint4 km[2], vm[2];
@@ -336,18 +199,15 @@ __global__ void __launch_bounds__(64 * kWaves) attn_rows_kernel(AttnArgs a) {
     for (int h = 0; h < 2; ++h) {
       // a block past the last key is masked: any page in range will do
       const int key = key0 + h * kKvBlock;
-      const uint32_t blk = uint32_t(key < kv_seen ? key : key0) / kKvBlock;
-      const uint32_t col = blk / a.page_blocks;
-      const uint32_t page = min(uint32_t(table[col]), a.n_pages - 1);
-      const uint32_t tok = (blk - col * a.page_blocks) * kKvBlock;
-      const char* kb = kh + page * a.page_stride + tok * int64_t(a.token_stride);
-      const char* vb = vh + page * a.page_stride + tok * int64_t(a.token_stride);
+      const BlockPlace at = block_place(a, table, key < it.kv_seen ? key : key0);
+      const char* kb = kh + at.page * a.page_stride + at.token * int64_t(a.token_stride);
+      const char* vb = vh + at.page * a.page_stride + at.token * int64_t(a.token_stride);
       kr[h].load(kb + uint32_t(r16) * a.token_stride, q);
 #pragma unroll
       for (int j = 0; j < 4; ++j) vr.load(4 * h + j, vb + uint32_t(4 * q + j) * a.token_stride, r16);
       if constexpr (KIND != FQ_KV_BF16) {
-        km[h] = *reinterpret_cast<const uint4*>(kmh + page * a.meta_page_stride + tok + 4 * q);
-        vm[h] = *reinterpret_cast<const uint4*>(vmh + page * a.meta_page_stride + tok + 4 * q);
+        km[h] = *reinterpret_cast<const uint4*>(kmh + at.page * a.meta_page_stride + at.token + 4 * q);
+        vm[h] = *reinterpret_cast<const uint4*>(vmh + at.page * a.meta_page_stride + at.token + 4 * q);
       }
     }
     // scores, in powers of two
@@ -369,15 +229,14 @@ __global__ void __launch_bounds__(64 * kWaves) attn_rows_kernel(AttnArgs a) {
       }
     }
     // the mask, where the tile is not seen whole by every row
-    const bool whole = key0 + kKvTile - 1 <= p_lo &&
-                       (a.window == 0 || key0 > p0 + tok_hi - a.window || key0 + kKvTile <= a.sinks);
+    const bool whole = it.whole<kKvTile>(a, key0);
     uint32_t seen = 0xFFu;
     if (!whole) {
       seen = 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int key = key0 + (j >> 2) * kKvBlock + 4 * q + (j & 3);
-        const bool see = key <= pos && (key >= win_lo || key < a.sinks);
+        const bool see = mine.sees(a, key);
         seen |= uint32_t(see) << j;
         s[j] = see ? s[j] : kNegInf;
       }
@@ -421,22 +280,32 @@ __global__ void __launch_bounds__(64 * kWaves) attn_rows_kernel(AttnArgs a) {
     }
 #pragma unroll
     for (int c = 0; c < CB; ++c) acc[c] *= shrink;
-    const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, pw);
-    bool clean = true;
-    if constexpr (KIND == FQ_KV_BF16) clean = whole || !has_nonfinite<D>(vr);
-    if (clean) {
+    if constexpr (KIND == FQ_KV_BF16) {
+      if (!whole) {
+        bool any = false;
 #pragma unroll
-      for (int c = 0; c < CB; ++c) acc[c] = mfma16(vr.operand(c), pb, acc[c]);
-    } else {
-      u32x4_t sw;
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
-      for (int i2 = 0; i2 < 4; ++i2)
-        sw[i2] = ((seen >> (2 * i2)) & 1u ? 0x3F80u : 0u) | ((seen >> (2 * i2 + 1)) & 1u ? 0x3F800000u : 0u);
-#pragma unroll
-      for (int c = 0; c < CB; ++c) {
-        const bf16x8_t v = take_nonfinite(vr.operand(c), sw, acc[c]);
-        acc[c] = mfma16(v, pb, acc[c]);
+          for (int w = 0; w < VRows<KIND, D>::W; ++w) {
+            any |= nonfinite_pair(vr.w[j][w]);
+            vr.w[j][w] = finite_pair(vr.w[j][w]);
+          }
+        odd |= __any(any);
       }
+    }
+    const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, pw);
+#pragma unroll
+    for (int c = 0; c < CB; ++c) acc[c] = mfma16(vr.operand(c), pb, acc[c]);
+  }
+  if constexpr (KIND == FQ_KV_BF16) {
+    if (odd) {
+      walk_partial_tiles<kKvTile>(a, it, table, vh, it.i_lo + wave, kWaves, [&](int key, const uint16_t* v) {
+        if (!mine.in || !mine.sees(a, key)) return;
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[c][i] += if_nonfinite(v[(4 * q + i) * CB + c]);
+      });
     }
   }
 
@@ -475,14 +344,14 @@ __global__ void __launch_bounds__(64 * kWaves) attn_rows_kernel(AttnArgs a) {
     for (int c = 0; c < CB; ++c) o[c] = fmaf(f, src[c], o[c]);
   }
 
-  if (n_parts > 1) {
+  if (it.n_parts > 1) {
     // partial sums: [item][range][row][D] floats, then [item][range][row][2]
-    const int64_t item = (int64_t(seq) * gridDim.y + head) * a.row_blocks + rb;
+    const int64_t item = (int64_t(it.seq) * gridDim.y + it.head) * a.row_blocks + it.rb;
     const uint32_t part_words = uint32_t(a.part_rows) * (D + 4);
     float* base_p = a.partials + item * a.split * part_words;
     const __amdgpu_buffer_rsrc_t prs = make_rsrc(base_p, uint32_t(a.split) * part_words * 4u);
-    if (row < rows) {
-      const uint32_t at = (uint32_t(sp) * part_words + uint32_t(row) * (D + 4)) * 4u;
+    if (row < it.rows) {
+      const uint32_t at = (uint32_t(it.part) * part_words + uint32_t(row) * (D + 4)) * 4u;
 #pragma unroll
       for (int c = 0; c < CB; c += 4)
         __builtin_amdgcn_raw_buffer_store_b128(
@@ -495,18 +364,18 @@ __global__ void __launch_bounds__(64 * kWaves) attn_rows_kernel(AttnArgs a) {
     __syncthreads();
     if (tid == 0) {
       const uint32_t old = __hip_atomic_fetch_add(a.counters + item, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      last_flag = old == uint32_t(n_parts - 1);
+      last_flag = old == uint32_t(it.n_parts - 1);
     }
     __syncthreads();
     if (!last_flag) return;
     if (tid == 0) __hip_atomic_store(a.counters + item, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (row >= rows) return;
+    if (row >= it.rows) return;
     // the last to arrive adds the ranges in their order
     mx = kNegInf;
     sum = 0.f;
 #pragma unroll
     for (int c = 0; c < CB; ++c) o[c] = 0.f;
-    for (int s2 = 0; s2 < n_parts; ++s2) {
+    for (int s2 = 0; s2 < it.n_parts; ++s2) {
       const uint32_t at = (uint32_t(s2) * part_words + uint32_t(row) * (D + 4)) * 4u;
       const f32x4_t ms = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(prs, int(at + D * 4u), 0, kSc1));
       const float m2 = fmaxf(mx, ms[0]);
@@ -523,12 +392,11 @@ __global__ void __launch_bounds__(64 * kWaves) attn_rows_kernel(AttnArgs a) {
       }
     }
   }
-  if (row >= rows) return;
-  const int64_t r = row0 + row;
-  const int tok = int(r / a.group);
-  const int oh = head * a.group + int(r - int64_t(tok) * a.group);
+  if (row >= it.rows) return;
+  Row dst;
+  dst.set(a, it, row);
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  uint16_t* op = a.O + (t0 + tok) * a.o_token + oh * a.o_head + ch;
+  uint16_t* op = a.O + (it.t0 + dst.token) * a.o_token + dst.head * a.o_head + ch;
   uint32_t w[CB / 2];
 #pragma unroll
   for (int c = 0; c < CB; c += 2)
@@ -536,7 +404,7 @@ __global__ void __launch_bounds__(64 * kWaves) attn_rows_kernel(AttnArgs a) {
   if constexpr (CB == 8) *reinterpret_cast<uint4*>(op) = uint4{w[0], w[1], w[2], w[3]};
   else *reinterpret_cast<uint2*>(op) = uint2{w[0], w[1]};
   if (a.lse && (tid & 15) == 0)
-    a.lse[(t0 + tok) * a.n_heads + oh] = sum == 0.f ? kNegInf : (mx + __log2f(sum)) * 0.69314718055994530942f;
+    a.lse[(it.t0 + dst.token) * a.n_heads + dst.head] = sum == 0.f ? kNegInf : (mx + __log2f(sum)) * 0.69314718055994530942f;
 }
 
 }  // namespace
@@ -549,6 +417,9 @@ namespace {
 
 constexpr int kTargetWorkgroups = 1024;   // four to a CU
 constexpr int kMinSplitTiles = 8;         // 256 keys a range: two tiles a wave
+constexpr int kTilesMinRows = 32;         // more rows: the kernel for many rows
+constexpr int kTargetTileWorkgroups = 512;
+constexpr int kMinSplitBigTiles = 4;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -556,27 +427,35 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 bool plan_attention(const fq_attention& a, const fq_kv_cache& c, AttnPlan* pl) {
   const int64_t group = a.n_heads / c.n_kv_heads;
-  const int64_t row_blocks = ceil_div(a.max_q * group, 16);
+  const int64_t rows = a.max_q * group;
+  pl->kernel = rows > kTilesMinRows ? FQ_ATTN_TILES : FQ_ATTN_ROWS;
+  pl->rows = pl->kernel == FQ_ATTN_TILES ? kTilesRows : 16;
+  pl->tile = pl->kernel == FQ_ATTN_TILES ? kTilesKeys : kKvTile;
+  const int64_t row_blocks = ceil_div(rows, pl->rows);
   if (row_blocks > (1 << 24) || a.n_seqs > 65535) return false;
-  pl->rows = 16;
   pl->row_blocks = int(row_blocks);
   const int64_t items = row_blocks * c.n_kv_heads * a.n_seqs;
-  // tiles that a block of rows can see at most
-  int64_t tiles = ceil_div(a.max_kv, kKvTile);
+  // tiles that a block of rows can see at most: those of the first keys, and a window of
+  // every token of the block, at any place
+  int64_t tiles = ceil_div(a.max_kv, pl->tile);
   if (a.window > 0)
-    tiles = std::min<int64_t>(tiles, ceil_div(a.window + ceil_div(16, group), kKvTile) + 2 + ceil_div(a.sinks, kKvTile));
+    tiles = std::min<int64_t>(tiles, ceil_div(a.window + ceil_div(pl->rows, group), pl->tile) + 2 +
+                                         ceil_div(a.sinks, pl->tile));
   // enough ranges to fill the GPU, none of them short; every item has a counter
+  const int64_t target = pl->kernel == FQ_ATTN_TILES ? kTargetTileWorkgroups : kTargetWorkgroups;
+  const int64_t shortest = pl->kernel == FQ_ATTN_TILES ? kMinSplitBigTiles : kMinSplitTiles;
   int64_t split = 1;
-  if (items <= kMaxStrips && items < kTargetWorkgroups)
-    split = std::max<int64_t>(1, std::min(ceil_div(kTargetWorkgroups, items), tiles / kMinSplitTiles));
+  if (items <= kMaxStrips && items < target)
+    split = std::max<int64_t>(1, std::min(ceil_div(target, items), tiles / shortest));
   pl->split_tiles = int(ceil_div(tiles, split));
   pl->split = int(ceil_div(tiles, pl->split_tiles));
   if (pl->split * row_blocks > INT32_MAX) return false;
   pl->workgroups = items * pl->split;
   if (pl->workgroups > INT32_MAX) return false;
-  pl->lds_bytes = c.head_dim == 64 ? fqk::kAttnLds<64> : fqk::kAttnLds<128>;
-  const int part_rows = int(std::min<int64_t>(16, a.max_q * group));
-  pl->partial_bytes = pl->split > 1 ? size_t(items) * pl->split * part_rows * (c.head_dim + 4) * 4 : 0;
+  if (pl->kernel == FQ_ATTN_TILES) pl->lds_bytes = fqk::attn_tiles_lds(c.head_dim);
+  else pl->lds_bytes = c.head_dim == 64 ? fqk::kAttnLds<64> : fqk::kAttnLds<128>;
+  pl->part_rows = int(std::min<int64_t>(pl->rows, rows));
+  pl->partial_bytes = pl->split > 1 ? size_t(items) * pl->split * pl->part_rows * (c.head_dim + 4) * 4 : 0;
   pl->ws_bytes = kCounterRegion + pl->partial_bytes;
   return true;
 }
@@ -611,6 +490,7 @@ int launch_attention(const AttnPlan& pl, const fq_attention& a, const fq_kv_cach
   g.total_q = a.total_q;
   g.token_stride = uint32_t(c.token_stride);
   g.page_blocks = uint32_t(c.page_size / kKvBlock);
+  g.page_magic = ((uint64_t(1) << 36) + g.page_blocks - 1) / g.page_blocks;
   g.n_pages = uint32_t(c.n_pages);
   g.group = group;
   g.n_heads = a.n_heads;
@@ -621,10 +501,11 @@ int launch_attention(const AttnPlan& pl, const fq_attention& a, const fq_kv_cach
   g.row_blocks = pl.row_blocks;
   g.split = pl.split;
   g.split_tiles = pl.split_tiles;
-  g.part_rows = int(std::min<int64_t>(16, int64_t(a.max_q) * group));
+  g.part_rows = pl.part_rows;
   g.scale_log2 = a.scale * 1.44269504088896340736f;
   const dim3 grid(unsigned(pl.row_blocks * pl.split), unsigned(c.n_kv_heads), unsigned(a.n_seqs));
   const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (pl.kernel == FQ_ATTN_TILES) return fqk::launch_attn_tiles(g, c.kind, c.head_dim, grid, s);
   auto go = [&](auto kind) {
     if (c.head_dim == 64)
       hipLaunchKernelGGL((fqk::attn_rows_kernel<kind.value, 64>), grid, dim3(64 * fqk::kWaves), pl.lds_bytes, s, g);

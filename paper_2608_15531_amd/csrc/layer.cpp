@@ -62,8 +62,8 @@ fq_status check_attention(const fq_attention* a, const fq_kv_cache* c) {
   if (!is_stride(a->q_token_stride, 8) || !is_stride(a->q_head_stride, 8) ||
       !is_stride(a->o_token_stride, 8) || !is_stride(a->o_head_stride, 8))
     return FQ_ERR_ALIGN;
-  // positions and key numbers are 32 bits wide, with a tile to spare
-  if (a->max_kv > INT32_MAX - 65536 || a->max_q > INT32_MAX - 65536) return FQ_ERR_UNSUPPORTED;
+  // key numbers below 2^28 (the kernels' division by the page size), positions 32 bits wide
+  if (a->max_kv > (1 << 28) || a->max_q > (1 << 28)) return FQ_ERR_UNSUPPORTED;
   return FQ_OK;
 }
 
@@ -122,12 +122,11 @@ fq_status fq_paged_attention_launch(const fq_attention* a, const fq_kv_cache* ca
   if (st != FQ_OK) return st;
   fqi::AttnPlan pl;
   if (!fqi::plan_attention(*a, *cache, &pl)) return FQ_ERR_UNSUPPORTED;
-  out[0] = FQ_ATTN_ROWS;
+  out[0] = pl.kernel;
   out[1] = pl.rows;
   out[2] = pl.row_blocks;
   out[3] = pl.split;
-  out[4] = int32_t(int64_t(pl.split_tiles) * fqi::kKvTile > INT32_MAX ? INT32_MAX
-                                                                      : pl.split_tiles * fqi::kKvTile);
+  out[4] = pl.split_tiles * pl.tile;   // max_kv <= 2^28
   out[5] = int32_t(pl.workgroups);
   out[6] = int32_t(pl.lds_bytes);
   out[7] = int32_t((pl.partial_bytes + 1023) >> 10);

@@ -13,13 +13,19 @@ namespace fqi {
 // are a tile of keys.
 constexpr int kKvBlock = 16;
 constexpr int kKvTile = 2 * kKvBlock;
+// Rows and keys of a workgroup's tile in the kernel for many rows.
+constexpr int kTilesRows = 128;
+constexpr int kTilesKeys = 64;
 
 // Launch plan of one attention call, from the sizes alone.
 struct AttnPlan {
+  int kernel;        // FQ_ATTN_*
   int rows;          // rows (token, query head) of a workgroup
   int row_blocks;    // of max_q tokens, per (sequence, KV head)
   int split;         // key ranges
-  int split_tiles;   // tiles of kKvTile keys in one
+  int tile;          // keys of a tile
+  int split_tiles;   // tiles in a range
+  int part_rows;     // rows of a partial result
   int64_t workgroups;
   size_t lds_bytes;
   size_t partial_bytes, ws_bytes;   // beyond the counters; with them

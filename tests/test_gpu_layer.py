@@ -374,8 +374,8 @@ def test_attention_extreme_scores(gpu_lib):
 
 
 def test_attention_bounds_above_the_lengths(gpu_lib):
-    """max_q and max_kv are bounds: larger ones change nothing but the rounding of the
-    joined ranges; tokens beyond max_q are left alone."""
+    """max_q and max_kv are bounds: larger ones change nothing but the kernel, the split and
+    with them the rounding; tokens beyond max_q are left alone."""
     fq = gpu_lib
     st = Step(fq, "int8", 128, 8, 2, 16, [1, 3], [100, 50], seed=2)
     wide = torch.full((2, 4096), -1, dtype=torch.int32)
@@ -389,7 +389,8 @@ def test_attention_bounds_above_the_lengths(gpu_lib):
     keep = torch.full_like(out, 9.0)
     fq.fq_paged_attention(st.q, st.cache, small, out=keep)
     torch.cuda.synchronize()
-    assert torch.equal(keep[:3], out[:3]) and (keep[3] == 9).all()
+    assert (keep[3] == 9).all()
+    st.check(torch.cat([keep[:3], out[3:]]), None, 0, 0)
 
 
 def test_attention_offsets_beyond_32_bits(gpu_lib):
