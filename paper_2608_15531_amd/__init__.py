@@ -12,7 +12,6 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
-import math
 import os
 import threading
 from dataclasses import dataclass
@@ -409,6 +408,22 @@ def _stream_handle(stream, device) -> int:
     return int(stream.cuda_stream)
 
 
+_raw_stream = None
+
+
+def _stream_of(stream, index: int) -> int:
+    """_stream_handle by device index, without making a torch Stream object of the current
+    stream (1.5 us a call) where torch offers its handle."""
+    global _raw_stream
+    if stream is not None:
+        return int(stream.cuda_stream)
+    if _raw_stream is None:
+        torch = _torch()
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda i: int(torch.cuda.current_stream(i).cuda_stream))
+    return _raw_stream(index)
+
+
 def workspace(nbytes: int, device, stream_handle: int):
     """Zero-filled workspace kept per (device, stream); the kernels leave it zeroed.
     Call it with the kernel's stream current (see _on_stream): the allocation
@@ -634,25 +649,31 @@ def fq_workspace_bytes_unfused(M: int, K: int, N: int, y_dtype=FQ_Y_BF16, split_
 
 # ------------------------------------------- the rest of a decoder layer --
 
-def _check_rows(t, dtype, shape, name):
-    """A CUDA tensor whose last dimension is contiguous; the others may have any stride."""
+def _check_rows(t, dtype, shape, name, index=None):
+    """The strides of a CUDA tensor whose last dimension is contiguous; the others may have
+    any.  index: the device that it has to be on."""
     if not isinstance(t, _torch().Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} "
                          f"{tuple(t.shape)}")
+    if index is not None and t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, not on device {index}")
     st = t.stride()
     if st[-1] != 1 and shape[-1] != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    if 1 in shape[:-1]:   # torch keeps any number as the stride of a dimension of one
+    if 1 in shape:   # torch keeps any number as the stride of a dimension of one
         st = tuple(0 if n == 1 else s for n, s in zip(shape, st))
     return st
 
 
-def _same_device(device, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, not on {device}")
+def _check_slots(slots, index):
+    if not isinstance(slots, _torch().Tensor) or slots.dim() != 1:
+        raise ValueError("slots: expected int64 [n_tokens]")
+    n = slots.shape[0]
+    if _check_rows(slots, _torch().int64, (n,), "slots", index)[0] != 1 and n > 1:
+        raise ValueError("slots must be contiguous")
+    return n
 
 
 class KVCache:
@@ -689,9 +710,12 @@ class KVCache:
             if (T > 1 and m[2] != 2) or m[0] % 2 or m[1] % 2:
                 raise ValueError("k_meta, v_meta: the tokens of a page must be contiguous")
             mst = (m[0] // 2, m[1] // 2, 1)
-        _same_device(k.device, v=v, k_meta=k_meta, v_meta=v_meta)
+        for t, name in ((v, "v"), (k_meta, "k_meta"), (v_meta, "v_meta")):
+            if t is not None and t.device != k.device:
+                raise ValueError(f"{name} is on {t.device}, k on {k.device}")
         self.k, self.v, self.k_meta, self.v_meta, self.kind = k, v, k_meta, v_meta, kind
         self.device = k.device
+        self._index = k.get_device()
         self.n_pages, self.n_kv_heads, self.page_size = P, H, T
         self.head_dim = 2 * row if kind == "int4" else row
         self._struct = fq_kv_cache(
@@ -743,11 +767,15 @@ class PagedBatch:
         if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
             raise ValueError("block_table: expected [n_seqs][pages]")
         st = _check_rows(block_table, torch.int32, (n, block_table.shape[1]), "block_table")
-        _same_device(cu_q.device, kv_lens=kv_lens, block_table=block_table)
+        for t, name in ((kv_lens, "kv_lens"), (block_table, "block_table")):
+            if t.device != cu_q.device:
+                raise ValueError(f"{name} is on {t.device}, cu_q on {cu_q.device}")
         self.cu_q, self.kv_lens, self.block_table = cu_q, kv_lens, block_table
         self.n_seqs, self.max_q, self.max_kv = n, int(max_q), int(max_kv)
         self.table_stride = st[0]
         self.device = cu_q.device
+        self._index = cu_q.get_device()
+        self._table_cols = block_table.shape[1]
         self._pointers = (cu_q.data_ptr(), kv_lens.data_ptr(), block_table.data_ptr())
 
 
@@ -755,48 +783,48 @@ def fq_kv_cache_write(cache: KVCache, k, v, slots, stream=None) -> None:
     """Store the rows k, v (bf16 [n_tokens][n_kv_heads][head_dim], any token and head
     stride) at `slots` (int64 [n_tokens]: page * page_size + place; a token whose slot is
     out of range, such as -1, is not stored), quantised as the cache's kind asks."""
-    torch = _torch()
-    shape = (slots.shape[0], cache.n_kv_heads, cache.head_dim)
-    ks = _check_rows(k, torch.bfloat16, shape, "k")
-    vs = _check_rows(v, torch.bfloat16, shape, "v")
-    _check_tensor(slots, torch.int64, shape[:1], "slots")
-    _same_device(cache.device, k=k, v=v, slots=slots)
-    _check(load().fq_kv_cache_write(cache._ref, k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0],
-                                    vs[1], slots.data_ptr(), shape[0],
-                                    _stream_handle(stream, cache.device)), "fq_kv_cache_write")
+    lib = load()
+    index, bf16 = cache._index, _torch().bfloat16
+    n = _check_slots(slots, index)
+    shape = (n, cache.n_kv_heads, cache.head_dim)
+    ks = _check_rows(k, bf16, shape, "k", index)
+    vs = _check_rows(v, bf16, shape, "v", index)
+    status = lib.fq_kv_cache_write(cache._ref, k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0],
+                                   vs[1], slots.data_ptr(), n, _stream_of(stream, index))
+    if status:
+        raise FqError(status, "fq_kv_cache_write")
 
 
 def fq_kv_cache_read(cache: KVCache, slots, k=None, v=None, dtype="bf16", stream=None):
     """The rows at `slots` (int64 [n_tokens]; out of range: zeros) as the values they
     stand for; returns K, V of [n_tokens][n_kv_heads][head_dim], bf16 or fp32 ("f32")."""
     torch = _torch()
+    lib = load()
+    index = cache._index
     f32 = dtype in ("f32", "fp32", torch.float32)
-    if not isinstance(slots, torch.Tensor) or slots.dim() != 1:
-        raise ValueError("slots: expected int64 [n_tokens]")
-    _check_tensor(slots, torch.int64, slots.shape, "slots")
-    shape = (slots.shape[0], cache.n_kv_heads, cache.head_dim)
+    n = _check_slots(slots, index)
+    shape = (n, cache.n_kv_heads, cache.head_dim)
     dt = torch.float32 if f32 else torch.bfloat16
-    with _on_stream(stream):
-        if k is None:
-            k = torch.empty(shape, dtype=dt, device=cache.device)
-        else:
-            _check_tensor(k, dt, shape, "k")
-        if v is None:
-            v = torch.empty(shape, dtype=dt, device=cache.device)
-        else:
-            _check_tensor(v, dt, shape, "v")
-    _same_device(cache.device, k=k, v=v, slots=slots)
-    _check(load().fq_kv_cache_read(cache._ref, slots.data_ptr(), shape[0], k.data_ptr(),
-                                   v.data_ptr(), FQ_Y_F32 if f32 else FQ_Y_BF16,
-                                   _stream_handle(stream, cache.device)), "fq_kv_cache_read")
+    for t, name in ((k, "k"), (v, "v")):
+        if t is not None:
+            _check_tensor(t, dt, shape, name)
+            _check_rows(t, dt, shape, name, index)
+    if k is None or v is None:
+        with _on_stream(stream):
+            k = torch.empty(shape, dtype=dt, device=cache.device) if k is None else k
+            v = torch.empty_like(k) if v is None else v
+    status = lib.fq_kv_cache_read(cache._ref, slots.data_ptr(), n, k.data_ptr(), v.data_ptr(),
+                                  FQ_Y_F32 if f32 else FQ_Y_BF16, _stream_of(stream, index))
+    if status:
+        raise FqError(status, "fq_kv_cache_read")
     return k, v
 
 
 def _attention(n_heads, q_strides, o_strides, total_q, cache, batch, scale, window, sinks):
     return fq_attention(batch.n_seqs, n_heads, batch.max_q, batch.max_kv, window, sinks, total_q,
                         q_strides[0], q_strides[1], o_strides[0], o_strides[1],
-                        batch.table_stride, batch.block_table.shape[1],
-                        1.0 / math.sqrt(cache.head_dim) if scale is None else scale)
+                        batch.table_stride, batch._table_cols,
+                        cache.head_dim ** -0.5 if scale is None else scale)
 
 
 def fq_paged_attention(q, cache: KVCache, batch: PagedBatch, scale: float | None = None,
@@ -813,39 +841,42 @@ def fq_paged_attention(q, cache: KVCache, batch: PagedBatch, scale: float | None
     lib = load()
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q: expected [total_q][n_heads][head_dim]")
-    shape = q.shape
-    device = cache.device
-    qs = _check_rows(q, torch.bfloat16, (shape[0], shape[1], cache.head_dim), "q")
-    _same_device(device, q=q, cu_q=batch.cu_q)
+    index, bf16 = cache._index, torch.bfloat16
+    total, heads, _ = q.shape
+    shape = (total, heads, cache.head_dim)
+    qs = _check_rows(q, bf16, shape, "q", index)
+    if batch._index != index:
+        raise ValueError(f"the batch is on {batch.device}, the cache on {cache.device}")
     lse = None
-    with _on_stream(stream):
-        if out is None:
-            out = torch.empty(shape, dtype=torch.bfloat16, device=device)
-        else:
-            _same_device(device, out=out)
-        if return_lse:
-            lse = torch.empty(shape[:2], dtype=torch.float32, device=device)
-    a = _attention(shape[1], qs, _check_rows(out, torch.bfloat16, shape, "out"), shape[0], cache,
-                   batch, scale, window, sinks)
-    ref = C.byref(a)
+    if out is not None:
+        os_ = _check_rows(out, bf16, shape, "out", index)
+    if out is None or return_lse:
+        with _on_stream(stream):
+            if out is None:
+                out = torch.empty(shape, dtype=bf16, device=cache.device)
+                os_ = out.stride()
+            if return_lse:
+                lse = torch.empty((total, heads), dtype=torch.float32, device=cache.device)
+    ref = C.byref(_attention(heads, qs, os_, total, cache, batch, scale, window, sinks))
     cu, lens, table = batch._pointers
-    sh = _stream_handle(stream, device)
-
-    def call(w):
-        return lib.fq_paged_attention(ref, q.data_ptr(), cache._ref, cu, lens, table,
-                                      out.data_ptr(), None if lse is None else lse.data_ptr(),
-                                      None if w is None else w.data_ptr(),
-                                      0 if w is None else w.numel(), sh)
-
-    status = call(ws if ws is not None else _workspaces.get((device.index, sh)))
+    sh = _stream_of(stream, index)
+    pq, po = q.data_ptr(), out.data_ptr()
+    pl = None if lse is None else lse.data_ptr()
+    w = _workspaces.get((index, sh)) if ws is None else ws
+    status = lib.fq_paged_attention(ref, pq, cache._ref, cu, lens, table, po, pl,
+                                    None if w is None else w.data_ptr(),
+                                    0 if w is None else w.numel(), sh)
     if status == _FQ_ERR_WORKSPACE and ws is None:
         # checked before anything is enqueued: none is kept yet, or too small a one
         need = C.c_size_t(0)
         _check(lib.fq_paged_attention_workspace_bytes(ref, cache._ref, C.byref(need)),
                "fq_paged_attention_workspace_bytes")
         with _on_stream(stream):
-            status = call(workspace(need.value, device, sh))
-    _check(status, "fq_paged_attention")
+            w = workspace(need.value, cache.device, sh)
+        status = lib.fq_paged_attention(ref, pq, cache._ref, cu, lens, table, po, pl,
+                                        w.data_ptr(), w.numel(), sh)
+    if status:
+        raise FqError(status, "fq_paged_attention")
     return (out, lse) if return_lse else out
 
 
@@ -893,36 +924,45 @@ def fq_gated_residual_norm(x, residual=None, pre_weight=None, post_weight=None, 
     lib = load()
     if not isinstance(x, torch.Tensor) or x.dim() != 2:
         raise ValueError("x: expected [rows][cols]")
-    shape = x.shape
+    index, bf16, shape, xt = x.get_device(), torch.bfloat16, x.shape, x.dtype
     M, H = shape
-    xs = _check_rows(x, x.dtype, shape, "x")
-    rt = x.dtype if residual is None else residual.dtype
-    n = fq_norm(M, H, _dtype_code(x.dtype, "x"), _dtype_code(rt, "residual"), eps, residual_scale,
-                xs[0], 0, 0, 0, 0)
+    xs = _check_rows(x, xt, shape, "x")
+    rt, rs, gs, pr, pg = xt, 0, 0, None, None
     if residual is not None:
-        n.residual_stride = _check_rows(residual, rt, shape, "residual")[0]
+        rt = residual.dtype
+        rs = _check_rows(residual, rt, shape, "residual", index)[0]
+        pr = residual.data_ptr()
     if gate is not None:
         if gate.dim() == 1:
-            _check_rows(gate, torch.bfloat16, (H,), "gate")
+            _check_rows(gate, bf16, (H,), "gate", index)
         else:
-            n.gate_stride = _check_rows(gate, torch.bfloat16, shape, "gate")[0]
-    for w, name in ((post_weight, "post_weight"), (pre_weight, "pre_weight")):
-        if w is not None:
-            _check_rows(w, torch.bfloat16, (H,), name)
-    with _on_stream(stream):
-        if residual_out is None:
-            residual_out = torch.empty(shape, dtype=rt, device=x.device)
-        if h is None and pre_weight is not None:
-            h = torch.empty(shape, dtype=torch.bfloat16, device=x.device)
-    n.residual_out_stride = _check_rows(residual_out, rt, shape, "residual_out")[0]
+            gs = _check_rows(gate, bf16, shape, "gate", index)[0]
+        pg = gate.data_ptr()
+    if post_weight is not None:
+        _check_rows(post_weight, bf16, (H,), "post_weight", index)
+    if pre_weight is not None:
+        _check_rows(pre_weight, bf16, (H,), "pre_weight", index)
+    elif h is not None:
+        raise ValueError("h needs pre_weight")
+    ros = hs = H
+    if residual_out is not None:
+        ros = _check_rows(residual_out, rt, shape, "residual_out", index)[0]
     if h is not None:
-        n.h_stride = _check_rows(h, torch.bfloat16, shape, "h")[0]
-    _same_device(x.device, residual=residual, pre_weight=pre_weight, post_weight=post_weight,
-                 gate=gate, residual_out=residual_out, h=h)
-    ptr = [None if t is None else t.data_ptr()
-           for t in (residual, post_weight, gate, pre_weight, residual_out, h)]
-    _check(lib.fq_gated_residual_norm(C.byref(n), x.data_ptr(), *ptr,
-                                      _stream_handle(stream, x.device)), "fq_gated_residual_norm")
+        hs = _check_rows(h, bf16, shape, "h", index)[0]
+    if residual_out is None or (h is None and pre_weight is not None):
+        with _on_stream(stream):
+            if residual_out is None:
+                residual_out = torch.empty(shape, dtype=rt, device=x.device)
+            if h is None and pre_weight is not None:
+                h = torch.empty(shape, dtype=bf16, device=x.device)
+    n = fq_norm(M, H, _dtype_code(xt, "x"), _dtype_code(rt, "residual"), eps, residual_scale, xs[0],
+                rs, gs, ros, hs)
+    status = lib.fq_gated_residual_norm(
+        C.byref(n), x.data_ptr(), pr, None if post_weight is None else post_weight.data_ptr(), pg,
+        None if pre_weight is None else pre_weight.data_ptr(), residual_out.data_ptr(),
+        None if h is None else h.data_ptr(), _stream_of(stream, index))
+    if status:
+        raise FqError(status, "fq_gated_residual_norm")
     return residual_out, h
 
 

@@ -346,7 +346,7 @@ __global__ void __launch_bounds__(64 * kWaves) attn_rows_kernel(AttnArgs a) {
 
   if (it.n_parts > 1) {
     // partial sums: [item][range][row][D] floats, then [item][range][row][2]
-    const int64_t item = (int64_t(it.seq) * gridDim.y + it.head) * a.row_blocks + it.rb;
+    const int64_t item = (int64_t(it.seq) * a.n_kv_heads + it.head) * a.row_blocks + it.rb;
     const uint32_t part_words = uint32_t(a.part_rows) * (D + 4);
     float* base_p = a.partials + item * a.split * part_words;
     const __amdgpu_buffer_rsrc_t prs = make_rsrc(base_p, uint32_t(a.split) * part_words * 4u);
@@ -449,7 +449,7 @@ bool plan_attention(const fq_attention& a, const fq_kv_cache& c, AttnPlan* pl) {
     split = std::max<int64_t>(1, std::min(ceil_div(target, items), tiles / shortest));
   pl->split_tiles = int(ceil_div(tiles, split));
   pl->split = int(ceil_div(tiles, pl->split_tiles));
-  if (pl->split * row_blocks > INT32_MAX) return false;
+  if (pl->split * row_blocks * c.n_kv_heads > INT32_MAX) return false;
   pl->workgroups = items * pl->split;
   if (pl->workgroups > INT32_MAX) return false;
   if (pl->kernel == FQ_ATTN_TILES) pl->lds_bytes = fqk::attn_tiles_lds(c.head_dim);
@@ -494,6 +494,7 @@ int launch_attention(const AttnPlan& pl, const fq_attention& a, const fq_kv_cach
   g.n_pages = uint32_t(c.n_pages);
   g.group = group;
   g.n_heads = a.n_heads;
+  g.n_kv_heads = c.n_kv_heads;
   g.max_q = a.max_q;
   g.max_kv = a.max_kv;
   g.window = a.window;
@@ -503,7 +504,7 @@ int launch_attention(const AttnPlan& pl, const fq_attention& a, const fq_kv_cach
   g.split_tiles = pl.split_tiles;
   g.part_rows = pl.part_rows;
   g.scale_log2 = a.scale * 1.44269504088896340736f;
-  const dim3 grid(unsigned(pl.row_blocks * pl.split), unsigned(c.n_kv_heads), unsigned(a.n_seqs));
+  const dim3 grid(unsigned(int64_t(pl.row_blocks) * pl.split * c.n_kv_heads), unsigned(a.n_seqs));
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (pl.kernel == FQ_ATTN_TILES) return fqk::launch_attn_tiles(g, c.kind, c.head_dim, grid, s);
   auto go = [&](auto kind) {

@@ -35,7 +35,7 @@ struct AttnArgs {
   uint64_t page_magic;     // ceil(2^36 / page_blocks): block / page_blocks by one product
   uint32_t n_pages;
   int group;               // query heads per KV head
-  int n_heads;
+  int n_heads, n_kv_heads;
   int max_q, max_kv, window, sinks;
   int row_blocks, split, split_tiles, part_rows;
   float scale_log2;        // scale * log2(e): the softmax runs in powers of two
@@ -60,7 +60,11 @@ struct BlockPlace {
 __device__ __forceinline__ BlockPlace block_place(const AttnArgs& a, const int32_t* table, int key) {
   const uint32_t blk = uint32_t(key) / kKvBlock;
   const uint32_t col = uint32_t((uint64_t(blk) * a.page_magic) >> 36);
-  return BlockPlace{min(uint32_t(table[col]), a.n_pages - 1), (blk - col * a.page_blocks) * kKvBlock};
+  // (as constant memory, so that it is a scalar load: among vector loads, waiting for it
+  // would wait for those before it)
+  typedef __attribute__((address_space(4))) const uint32_t constant_u32;
+  const uint32_t page = reinterpret_cast<constant_u32*>(reinterpret_cast<uintptr_t>(table))[col];
+  return BlockPlace{min(page, a.n_pages - 1), (blk - col * a.page_blocks) * kKvBlock};
 }
 
 // Which tiles a block of rows at positions [p_lo, p_hi] sees: with a window, the tiles of
@@ -89,6 +93,12 @@ __device__ __forceinline__ TileRange tile_range(int p_lo, int p_hi, int window, 
 
 // What a workgroup works on: a block of ROWS rows of one (sequence, KV head), one range of
 // the key tiles that the block sees.
+//
+// KV heads vary fastest over the workgroups, which go to the eight XCDs in turn: the
+// blocks and ranges that read the same keys meet in one L2 (with 8 KV heads, or any
+// multiple or divisor).  The last rows, which see the most keys, come first.  Empty
+// workgroups (past a shorter sequence's rows or keys) lie together rather than in turn
+// with others, which would leave whole shader engines idle.
 struct Item {
   int head, seq, rb, part, n_parts;
   int64_t t0;          // first new token of the sequence
@@ -103,10 +113,11 @@ struct Item {
 
   template <int ROWS, int TILE>
   __device__ __forceinline__ bool set(const AttnArgs& a) {
-    rb = int(blockIdx.x) % a.row_blocks;
-    part = int(blockIdx.x) / a.row_blocks;
-    head = int(blockIdx.y);
-    seq = int(blockIdx.z);
+    head = int(blockIdx.x) % a.n_kv_heads;
+    const int x = int(blockIdx.x) / a.n_kv_heads;
+    part = x % a.split;
+    rb = a.row_blocks - 1 - x / a.split;
+    seq = int(blockIdx.y);
     t0 = min(max(int64_t(a.cu_q[seq]), int64_t(0)), a.total_q);
     const int64_t t1 = min(max(int64_t(a.cu_q[seq + 1]), t0), a.total_q);
     const int q_all = int(t1 - t0);               // before the bound: positions count from the end

@@ -182,6 +182,22 @@ __device__ __forceinline__ uint2 read_transposed(uint32_t lds) {
   return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4*>(uintptr_t(lds))));
 }
 
+// The order of a stretch of N products: each one's R operand reads are AHEAD products
+// earlier, PRE vector operations come before the first and V after each.  (The compiler
+// alone puts each read right before its product, and the wave then waits for LDS.)
+template <int N, int R, int AHEAD, int PRE, int V>
+__device__ __forceinline__ void order_products() {
+  constexpr int kMfma = 0x8, kDsRead = 0x100, kValu = 0x2, kTrans = 0x400;
+  __builtin_amdgcn_sched_group_barrier(kDsRead, R * AHEAD, 0);
+  if constexpr (PRE > 0) __builtin_amdgcn_sched_group_barrier(kValu | kTrans, PRE, 0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+    if (i + AHEAD < N) __builtin_amdgcn_sched_group_barrier(kDsRead, R, 0);
+    if constexpr (V > 0) __builtin_amdgcn_sched_group_barrier(kValu | kTrans, V, 0);
+  }
+}
+
 template <int KIND, int D>
 __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs a) {
   constexpr int STEPS = D / 16, DB = D / 32;
@@ -204,6 +220,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
   // softmax in powers of two of |scale|; a negative scale changes the sign of q, 0 makes it 0
   const uint32_t q_sign = a.scale_log2 < 0.f ? 0x80008000u : 0u;
   const float c2 = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
+  const float grow = 8.f / c2;
   const bool use_q = mine.in && a.scale_log2 != 0.f;
   const uint16_t* qp = a.Q + (it.t0 + mine.token) * a.q_token + mine.head * a.q_head;
   bf16x8_t qv[STEPS];
@@ -294,6 +311,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
 #pragma unroll
         for (int st = 0; st < STEPS; ++st)
           s[kb] = mfma32(lds_read16(k_at[st] + at, kb * 32 * 2 * D), qv[st], s[kb]);
+      order_products<2 * STEPS, 1, 4, 0, 0>();
       if constexpr (KIND != FQ_KV_BF16) {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
@@ -326,7 +344,9 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
 #pragma unroll
         for (int j = 0; j < 16; ++j) top = fmaxf(top, s[kb][j]);
       top = pair_max(top);
-      if (__any(top > m)) {
+      // the sums move to a new maximum only when some row's has grown by more than 2^8: until
+      // then its weights are up to 2^8, which fp32 sums and bf16 weights hold as well
+      if (__any(top > m + grow)) {
         const float m_new = fmaxf(m, top);
         const float shrink = __builtin_amdgcn_exp2f((m - (m_new == kNegInf ? 0.f : m_new)) * c2);
         m = m_new;
@@ -366,6 +386,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
           acc[c] = mfma32(__builtin_bit_cast(bf16x8_t, u32x4_t{lo.x, lo.y, hi.x, hi.y}), pb, acc[c]);
         }
       }
+      order_products<4 * DB, 2, 4, 28, 7>();
     }
     if (more) {
       share.store(tile_lds + (buf ^ 1) * TileLds<D>::one, tid);
@@ -390,7 +411,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
   l = pair_add(l);
   if (it.n_parts > 1) {
     // partial sums: [item][range][row][D + 4] floats, the last four: m c2, l
-    const int64_t item = (int64_t(it.seq) * gridDim.y + it.head) * a.row_blocks + it.rb;
+    const int64_t item = (int64_t(it.seq) * a.n_kv_heads + it.head) * a.row_blocks + it.rb;
     const uint32_t part_words = uint32_t(a.part_rows) * (D + 4);
     const __amdgpu_buffer_rsrc_t prs =
         make_rsrc(a.partials + item * a.split * part_words, uint32_t(a.split) * part_words * 4u);
