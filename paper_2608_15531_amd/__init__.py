@@ -662,18 +662,32 @@ def _check_rows(t, dtype, shape, name, index=None):
     st = t.stride()
     if st[-1] != 1 and shape[-1] != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    if 1 in shape:   # torch keeps any number as the stride of a dimension of one
-        st = tuple(0 if n == 1 else s for n, s in zip(shape, st))
     return st
+
+
+def _rows(t, dtype, shape, name, index):
+    """_check_rows, quick where all is well."""
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == index:
+            st = t.stride()
+            if st[-1] == 1:
+                return st
+    except AttributeError:
+        pass   # no tensor
+    return _check_rows(t, dtype, shape, name, index)
 
 
 def _check_slots(slots, index):
     if not isinstance(slots, _torch().Tensor) or slots.dim() != 1:
         raise ValueError("slots: expected int64 [n_tokens]")
     n = slots.shape[0]
-    if _check_rows(slots, _torch().int64, (n,), "slots", index)[0] != 1 and n > 1:
-        raise ValueError("slots must be contiguous")
+    _rows(slots, _torch().int64, (n,), "slots", index)
     return n
+
+
+def _any_stride(t):
+    """Strides with 0 for dimensions of one, of which torch keeps any number."""
+    return tuple(0 if n == 1 else s for n, s in zip(t.shape, t.stride()))
 
 
 class KVCache:
@@ -692,8 +706,10 @@ class KVCache:
         dtype = torch.bfloat16 if kind == "bf16" else torch.uint8
         if not isinstance(k, torch.Tensor) or k.dim() != 4:
             raise ValueError("k: expected [n_pages][n_kv_heads][page_size][row]")
-        st = _check_rows(k, dtype, k.shape, "k")
-        if _check_rows(v, dtype, k.shape, "v") != st:
+        _check_rows(k, dtype, k.shape, "k")
+        _check_rows(v, dtype, k.shape, "v")
+        st = _any_stride(k)
+        if _any_stride(v) != st:
             raise ValueError("k and v must have the same strides")
         P, H, T, row = k.shape
         size = k.element_size()
@@ -704,8 +720,10 @@ class KVCache:
         else:
             if k_meta is None or v_meta is None:
                 raise ValueError(f"a cache of kind {kind} needs k_meta and v_meta")
-            m = _check_rows(k_meta, torch.bfloat16, (P, H, T, 2), "k_meta")
-            if _check_rows(v_meta, torch.bfloat16, (P, H, T, 2), "v_meta") != m:
+            _check_rows(k_meta, torch.bfloat16, (P, H, T, 2), "k_meta")
+            _check_rows(v_meta, torch.bfloat16, (P, H, T, 2), "v_meta")
+            m = _any_stride(k_meta)
+            if _any_stride(v_meta) != m:
                 raise ValueError("k_meta and v_meta must have the same strides")
             if (T > 1 and m[2] != 2) or m[0] % 2 or m[1] % 2:
                 raise ValueError("k_meta, v_meta: the tokens of a page must be contiguous")
@@ -766,7 +784,8 @@ class PagedBatch:
         _check_tensor(cu_q, torch.int32, (n + 1,), "cu_q")
         if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
             raise ValueError("block_table: expected [n_seqs][pages]")
-        st = _check_rows(block_table, torch.int32, (n, block_table.shape[1]), "block_table")
+        _check_rows(block_table, torch.int32, (n, block_table.shape[1]), "block_table")
+        st = _any_stride(block_table)
         for t, name in ((kv_lens, "kv_lens"), (block_table, "block_table")):
             if t.device != cu_q.device:
                 raise ValueError(f"{name} is on {t.device}, cu_q on {cu_q.device}")
@@ -787,8 +806,8 @@ def fq_kv_cache_write(cache: KVCache, k, v, slots, stream=None) -> None:
     index, bf16 = cache._index, _torch().bfloat16
     n = _check_slots(slots, index)
     shape = (n, cache.n_kv_heads, cache.head_dim)
-    ks = _check_rows(k, bf16, shape, "k", index)
-    vs = _check_rows(v, bf16, shape, "v", index)
+    ks = _rows(k, bf16, shape, "k", index)
+    vs = _rows(v, bf16, shape, "v", index)
     status = lib.fq_kv_cache_write(cache._ref, k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0],
                                    vs[1], slots.data_ptr(), n, _stream_of(stream, index))
     if status:
@@ -808,7 +827,7 @@ def fq_kv_cache_read(cache: KVCache, slots, k=None, v=None, dtype="bf16", stream
     for t, name in ((k, "k"), (v, "v")):
         if t is not None:
             _check_tensor(t, dt, shape, name)
-            _check_rows(t, dt, shape, name, index)
+            _rows(t, dt, shape, name, index)
     if k is None or v is None:
         with _on_stream(stream):
             k = torch.empty(shape, dtype=dt, device=cache.device) if k is None else k
@@ -844,16 +863,16 @@ def fq_paged_attention(q, cache: KVCache, batch: PagedBatch, scale: float | None
     index, bf16 = cache._index, torch.bfloat16
     total, heads, _ = q.shape
     shape = (total, heads, cache.head_dim)
-    qs = _check_rows(q, bf16, shape, "q", index)
+    qs = _rows(q, bf16, shape, "q", index)
     if batch._index != index:
         raise ValueError(f"the batch is on {batch.device}, the cache on {cache.device}")
     lse = None
     if out is not None:
-        os_ = _check_rows(out, bf16, shape, "out", index)
+        os_ = _rows(out, bf16, shape, "out", index)
     if out is None or return_lse:
         with _on_stream(stream):
             if out is None:
-                out = torch.empty(shape, dtype=bf16, device=cache.device)
+                out = torch.empty_like(q, memory_format=torch.contiguous_format)
                 os_ = out.stride()
             if return_lse:
                 lse = torch.empty((total, heads), dtype=torch.float32, device=cache.device)
@@ -926,35 +945,38 @@ def fq_gated_residual_norm(x, residual=None, pre_weight=None, post_weight=None, 
         raise ValueError("x: expected [rows][cols]")
     index, bf16, shape, xt = x.get_device(), torch.bfloat16, x.shape, x.dtype
     M, H = shape
-    xs = _check_rows(x, xt, shape, "x")
+    xs = _rows(x, xt, shape, "x", index)
     rt, rs, gs, pr, pg = xt, 0, 0, None, None
     if residual is not None:
         rt = residual.dtype
-        rs = _check_rows(residual, rt, shape, "residual", index)[0]
+        rs = _rows(residual, rt, shape, "residual", index)[0]
         pr = residual.data_ptr()
     if gate is not None:
         if gate.dim() == 1:
-            _check_rows(gate, bf16, (H,), "gate", index)
+            _rows(gate, bf16, (H,), "gate", index)
         else:
-            gs = _check_rows(gate, bf16, shape, "gate", index)[0]
+            gs = _rows(gate, bf16, shape, "gate", index)[0]
         pg = gate.data_ptr()
     if post_weight is not None:
-        _check_rows(post_weight, bf16, (H,), "post_weight", index)
+        _rows(post_weight, bf16, (H,), "post_weight", index)
     if pre_weight is not None:
-        _check_rows(pre_weight, bf16, (H,), "pre_weight", index)
+        _rows(pre_weight, bf16, (H,), "pre_weight", index)
     elif h is not None:
         raise ValueError("h needs pre_weight")
     ros = hs = H
     if residual_out is not None:
-        ros = _check_rows(residual_out, rt, shape, "residual_out", index)[0]
+        ros = _rows(residual_out, rt, shape, "residual_out", index)[0]
     if h is not None:
-        hs = _check_rows(h, bf16, shape, "h", index)[0]
+        hs = _rows(h, bf16, shape, "h", index)[0]
     if residual_out is None or (h is None and pre_weight is not None):
         with _on_stream(stream):
+            like = torch.contiguous_format
             if residual_out is None:
-                residual_out = torch.empty(shape, dtype=rt, device=x.device)
+                residual_out = torch.empty_like(x if residual is None else residual,
+                                                memory_format=like)
             if h is None and pre_weight is not None:
-                h = torch.empty(shape, dtype=bf16, device=x.device)
+                h = torch.empty_like(x, memory_format=like) if xt is bf16 else \
+                    torch.empty(shape, dtype=bf16, device=x.device)
     n = fq_norm(M, H, _dtype_code(xt, "x"), _dtype_code(rt, "residual"), eps, residual_scale, xs[0],
                 rs, gs, ros, hs)
     status = lib.fq_gated_residual_norm(

@@ -29,14 +29,8 @@ namespace fqk {
 namespace {
 
 // Maximum and sum over the four lanes of a row (lanes l, l ^ 16, l ^ 32, l ^ 48).
-__device__ __forceinline__ float row_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
-}
-__device__ __forceinline__ float row_add(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
-}
+__device__ __forceinline__ float row_max(float v) { return across32(across16(v, Max{}), Max{}); }
+__device__ __forceinline__ float row_add(float v) { return across32(across16(v, Add{}), Add{}); }
 
 // Channels of the lane's 8 k-slots in product step `st` of S^T: the first of them.
 // They follow from the 16 (or 8) bytes of a K row that a lane loads at once.

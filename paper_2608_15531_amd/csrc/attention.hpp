@@ -8,6 +8,7 @@
 
 #include "device.hpp"
 #include "internal.hpp"
+#include "lanes.hpp"
 #include "layer.hpp"
 
 namespace fqk {

@@ -34,8 +34,8 @@ __device__ __forceinline__ f32x16_t mfma32(bf16x8_t a, bf16x8_t b, f32x16_t c) {
 }
 
 // Maximum and sum over lanes l and l ^ 32.
-__device__ __forceinline__ float pair_max(float v) { return fmaxf(v, __shfl_xor(v, 32)); }
-__device__ __forceinline__ float pair_add(float v) { return v + __shfl_xor(v, 32); }
+__device__ __forceinline__ float pair_max(float v) { return across32(v, Max{}); }
+__device__ __forceinline__ float pair_add(float v) { return across32(v, Add{}); }
 
 // Two f32 whose upper halves are exact bf16, as a pair.
 __device__ __forceinline__ uint32_t pack_exact(float lo, float hi) {

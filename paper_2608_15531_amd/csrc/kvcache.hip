@@ -1,13 +1,15 @@
 // The paged KV cache: rows quantised as they are written, and read back.
 //
 // A row's range needs all of its channels and nothing else, so D / 8 lanes hold one
-// row, 16 bytes of bf16 each, and agree on its range without LDS.  A workgroup takes
-// consecutive tokens of one head: in a page these rows follow one another, so the
-// stores of a workgroup fill whole cache lines, while each row's read is 128 or 256
-// contiguous bytes wherever it lies.  Both kernels are bound by memory.
+// row, 16 bytes of bf16 each, and agree on its range without LDS.  A thread takes K and V
+// of kTokens tokens of one head, all loads first: the chain slot, row, store is latency,
+// and several rows a thread hide it.  A workgroup takes consecutive tokens of one head: in
+// a page these rows follow one another, so their stores fill whole cache lines.  Both
+// kernels are bound by memory.
 #include <hip/hip_runtime.h>
 
 #include "device.hpp"
+#include "lanes.hpp"
 #include "layer.hpp"
 
 namespace fqk {
@@ -59,27 +61,19 @@ __device__ __forceinline__ float scale_of(float span) {
   return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, q) + 0xFFFFu) & 0xFFFF0000u);
 }
 
+constexpr int kTokens = 1;   // a thread
+
+// Quantises a row's 8 channels of this lane and stores them.  The quotients x / s are the
+// correctly rounded ones: of numbers of 8 bits they round to the same integer as the exact
+// quotients do, ties among them.  With r = 1 / s rounded correctly, y = x r and the exact
+// remainder e = x - y s, fma(e, r, y) is the rounded quotient (Markstein) as long as r and
+// e s are far from the ends of the range.
 template <int KIND, int D>
-__global__ void __launch_bounds__(256)
-kv_write_kernel(CacheArgs a, const uint16_t* K, const uint16_t* V, int64_t k_token, int64_t k_head,
-                int64_t v_token, int64_t v_head, const int64_t* slots, int n_tokens) {
-  constexpr int LPR = D / 8;   // lanes a row
-  const int t = int(blockIdx.x) * (256 / LPR) + int(threadIdx.x) / LPR;
-  const int i = int(threadIdx.x) % LPR;
-  const int head = int(blockIdx.y);
-  const int which = int(blockIdx.z);   // 0: K, 1: V
-  const bool in = t < n_tokens;
-  const int64_t slot = in ? slots[t] : -1;
-  const bool store = uint64_t(slot) < uint64_t(a.n_slots);
-  const uint16_t* src = (which ? V + head * v_head : K + head * k_head) + (which ? v_token : k_token) * int64_t(t);
-  uint4 w{0, 0, 0, 0};
-  if (store) w = reinterpret_cast<const uint4*>(src)[i];
-  const Place p = place_of(store ? slot : 0, a);
-  char* dst = a.rows[which] + p.page * a.page_stride + head * a.head_stride + int64_t(p.off) * a.token_stride;
+__device__ __forceinline__ void store_row(char* dst, uint32_t* meta, uint4 w, int i, bool store) {
   if constexpr (KIND == FQ_KV_BF16) {
     if (store) reinterpret_cast<uint4*>(dst)[i] = w;
-    return;
   } else {
+    constexpr int LPR = D / 8;
     float x[8];
     const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
     float hi = 0.f, lo = 0.f;
@@ -96,20 +90,30 @@ kv_write_kernel(CacheArgs a, const uint16_t* K, const uint16_t* V, int64_t k_tok
       lo = fminf(lo, x[j]);
     }
     if (odd) hi = __builtin_inff();
-#pragma unroll
-    for (int m = 1; m < LPR; m <<= 1) {
-      hi = fmaxf(hi, __shfl_xor(hi, m));
-      lo = fminf(lo, __shfl_xor(lo, m));
-    }
+    hi = over_lanes<LPR>(hi, Max{});
+    lo = over_lanes<LPR>(lo, Min{});
     const float span = hi - lo;
     const bool bad = !(span <= 3.4028234663852886e38f);
     const float s = scale_of<KIND>(bad ? 0.f : span);
     const float z = fminf(fmaxf(rintf(__fdiv_rn(-lo, s)), 0.f), kTop<KIND>);
     uint32_t c[8];
+    const bool middle = s > 0x1p-100f && s < 0x1p100f;
+    const float r = __fdiv_rn(1.f, s);
+    if (middle) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float q = fminf(fmaxf(rintf(__fdiv_rn(x[j], s)) + z, 0.f), kTop<KIND>);
-      c[j] = bad ? 0u : uint32_t(q);
+      for (int j = 0; j < 8; ++j) {
+        const float y = x[j] * r;
+        x[j] = fmaf(fmaf(-y, s, x[j]), r, y);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = __fdiv_rn(x[j], s);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c[j] = uint32_t(fminf(fmaxf(rintf(x[j]) + z, 0.f), kTop<KIND>));
+    if (bad) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) c[j] = 0u;
     }
     if (!store) return;
     if constexpr (KIND == FQ_KV_INT8) {
@@ -126,56 +130,138 @@ kv_write_kernel(CacheArgs a, const uint16_t* K, const uint16_t* V, int64_t k_tok
     if (i == 0) {
       const uint32_t zb = bad ? 0u : __builtin_bit_cast(uint32_t, z) & 0xFFFF0000u;
       const uint32_t sb = bad ? 0x7FC0u : __builtin_bit_cast(uint32_t, s) >> 16;
-      a.meta[which][p.page * a.meta_page_stride + head * a.meta_head_stride + p.off] = sb | zb;
+      *meta = sb | zb;
     }
   }
 }
 
-template <int KIND, int D, bool F32>
+template <int KIND, int D>
 __global__ void __launch_bounds__(256)
-kv_read_kernel(CacheArgs a, const int64_t* slots, int n_tokens, void* K, void* V) {
-  constexpr int LPR = D / 8;
-  const int t = int(blockIdx.x) * (256 / LPR) + int(threadIdx.x) / LPR;
+kv_write_kernel(CacheArgs a, const uint16_t* K, const uint16_t* V, int64_t k_token, int64_t k_head,
+                int64_t v_token, int64_t v_head, const int64_t* slots, int n_tokens) {
+  constexpr int LPR = D / 8, PER = 256 / LPR;   // lanes a row, rows of a workgroup at a time
   const int i = int(threadIdx.x) % LPR;
   const int head = int(blockIdx.y);
-  const int which = int(blockIdx.z);
-  if (t >= n_tokens) return;
-  const int64_t slot = slots[t];
-  const bool in = uint64_t(slot) < uint64_t(a.n_slots);
-  const Place p = place_of(in ? slot : 0, a);
-  const char* src = a.rows[which] + p.page * a.page_stride + head * a.head_stride + int64_t(p.off) * a.token_stride;
-  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (in) {
-    if constexpr (KIND == FQ_KV_BF16) {
-      const uint4 w = reinterpret_cast<const uint4*>(src)[i];
-      const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+  const int t0 = int(blockIdx.x) * (PER * kTokens) + int(threadIdx.x) / LPR;
+  int64_t slot[kTokens];
+  uint4 k[kTokens], v[kTokens];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        x[2 * j] = __builtin_bit_cast(float, ws[j] << 16);
-        x[2 * j + 1] = __builtin_bit_cast(float, ws[j] & 0xFFFF0000u);
+  for (int u = 0; u < kTokens; ++u) {
+    const int t = t0 + u * PER;
+    const bool in = t < n_tokens;
+    slot[u] = in ? slots[t] : -1;
+    k[u] = v[u] = uint4{0, 0, 0, 0};
+    if (in) {
+      k[u] = reinterpret_cast<const uint4*>(K + head * k_head + k_token * int64_t(t))[i];
+      v[u] = reinterpret_cast<const uint4*>(V + head * v_head + v_token * int64_t(t))[i];
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kTokens; ++u) {
+    const bool store = uint64_t(slot[u]) < uint64_t(a.n_slots);
+    const Place p = place_of(store ? slot[u] : 0, a);
+    const int64_t at = p.page * a.page_stride + head * a.head_stride + int64_t(p.off) * a.token_stride;
+    const int64_t word = p.page * a.meta_page_stride + head * a.meta_head_stride + p.off;
+    store_row<KIND, D>(a.rows[0] + at, a.meta[0] + word, k[u], i, store);
+    store_row<KIND, D>(a.rows[1] + at, a.meta[1] + word, v[u], i, store);
+  }
+}
+
+// N channels from channel c of a row on, as numbers.
+template <int KIND, int N>
+__device__ __forceinline__ void load_channels(const char* row, int c, uint32_t meta, float (&x)[N]) {
+  if constexpr (KIND == FQ_KV_BF16) {
+#pragma unroll
+    for (int j = 0; j < N / 4; ++j) {
+      const uint2 w = reinterpret_cast<const uint2*>(row + 2 * c)[j];
+      x[4 * j] = __builtin_bit_cast(float, w.x << 16);
+      x[4 * j + 1] = __builtin_bit_cast(float, w.x & 0xFFFF0000u);
+      x[4 * j + 2] = __builtin_bit_cast(float, w.y << 16);
+      x[4 * j + 3] = __builtin_bit_cast(float, w.y & 0xFFFF0000u);
+    }
+  } else {
+    const float s = __builtin_bit_cast(float, meta << 16), z = __builtin_bit_cast(float, meta & 0xFFFF0000u);
+    if constexpr (KIND == FQ_KV_INT8) {
+#pragma unroll
+      for (int j = 0; j < N / 4; ++j) {
+        const uint32_t w = reinterpret_cast<const uint32_t*>(row + c)[j];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * j + e] = s * (float((w >> (8 * e)) & 255u) - z);
       }
     } else {
-      const uint32_t m = a.meta[which][p.page * a.meta_page_stride + head * a.meta_head_stride + p.off];
-      const float s = __builtin_bit_cast(float, m << 16), z = __builtin_bit_cast(float, m & 0xFFFF0000u);
-      if constexpr (KIND == FQ_KV_INT8) {
-        const uint2 w = reinterpret_cast<const uint2*>(src)[i];
+      uint32_t w;
+      if constexpr (N == 8) w = *reinterpret_cast<const uint32_t*>(row + c / 2);
+      else w = *reinterpret_cast<const uint16_t*>(row + c / 2);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = s * (float(((j < 4 ? w.x : w.y) >> (8 * (j & 3))) & 255u) - z);
+      for (int e = 0; e < N; ++e) x[e] = s * (float((w >> (4 * e)) & 15u) - z);
+    }
+  }
+}
+
+// A 16-byte store; STREAM: past the caches, for outputs that do not fit them.
+template <bool STREAM, class T, class V>
+__device__ __forceinline__ void put(T* p, V v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<V*>(p));
+  else *reinterpret_cast<V*>(p) = v;
+}
+
+// A lane's channels: 8 in a row for bf16 out; for fp32 4 in each half of the row, so that
+// a store of 16 bytes a lane is contiguous over the lanes.
+template <int KIND, int D, bool F32, bool STREAM>
+__global__ void __launch_bounds__(256)
+kv_read_kernel(CacheArgs a, const int64_t* slots, int n_tokens, void* K, void* V) {
+  constexpr int LPR = D / 8, PER = 256 / LPR;
+  const int i = int(threadIdx.x) % LPR;
+  const int head = int(blockIdx.y);
+  const int t0 = int(blockIdx.x) * (PER * kTokens) + int(threadIdx.x) / LPR;
+  float x[kTokens][2][8];
+#pragma unroll
+  for (int u = 0; u < kTokens; ++u) {
+    const int t = t0 + u * PER;
+    const int64_t slot = t < n_tokens ? slots[t] : -1;
+    const bool in = uint64_t(slot) < uint64_t(a.n_slots);
+    const Place p = place_of(in ? slot : 0, a);
+    const int64_t at = p.page * a.page_stride + head * a.head_stride + int64_t(p.off) * a.token_stride;
+    const int64_t word = p.page * a.meta_page_stride + head * a.meta_head_stride + p.off;
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+      if (!in) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[u][v][j] = 0.f;
+        continue;
+      }
+      const uint32_t meta = KIND == FQ_KV_BF16 ? 0u : a.meta[v][word];
+      if constexpr (F32) {
+        float lo[4], hi[4];
+        load_channels<KIND, 4>(a.rows[v] + at, 4 * i, meta, lo);
+        load_channels<KIND, 4>(a.rows[v] + at, D / 2 + 4 * i, meta, hi);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[u][v][j] = lo[j];
+          x[u][v][4 + j] = hi[j];
+        }
       } else {
-        const uint32_t w = reinterpret_cast<const uint32_t*>(src)[i];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = s * (float((w >> (4 * j)) & 15u) - z);
+        load_channels<KIND, 8>(a.rows[v] + at, 8 * i, meta, x[u][v]);
       }
     }
   }
-  const int64_t at = (int64_t(t) * gridDim.y + head) * D + i * 8;
-  if constexpr (F32) {
-    float* o = static_cast<float*>(which ? V : K) + at;
-    reinterpret_cast<float4*>(o)[0] = float4{x[0], x[1], x[2], x[3]};
-    reinterpret_cast<float4*>(o)[1] = float4{x[4], x[5], x[6], x[7]};
-  } else {
-    uint16_t* o = static_cast<uint16_t*>(which ? V : K) + at;
-    *reinterpret_cast<uint4*>(o) = uint4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])};
+#pragma unroll
+  for (int u = 0; u < kTokens; ++u) {
+    const int t = t0 + u * PER;
+    if (t >= n_tokens) return;
+    const int64_t at = (int64_t(t) * gridDim.y + head) * D;
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+      const float* y = x[u][v];
+      if constexpr (F32) {
+        float* o = static_cast<float*>(v ? V : K) + at;
+        put<STREAM>(o + 4 * i, f32x4_t{y[0], y[1], y[2], y[3]});
+        put<STREAM>(o + D / 2 + 4 * i, f32x4_t{y[4], y[5], y[6], y[7]});
+      } else {
+        uint16_t* o = static_cast<uint16_t*>(v ? V : K) + at;
+        put<STREAM>(o + 8 * i, u32x4_t{pack2(y[0], y[1]), pack2(y[2], y[3]), pack2(y[4], y[5]), pack2(y[6], y[7])});
+      }
+    }
   }
 }
 
@@ -199,8 +285,8 @@ void by_kind(const fq_kv_cache& c, F&& f) {
 }
 
 dim3 token_grid(const fq_kv_cache& c, int64_t n_tokens) {
-  const int per = 256 / (c.head_dim / 8);
-  return dim3(unsigned((n_tokens + per - 1) / per), unsigned(c.n_kv_heads), 2);
+  const int per = 256 / (c.head_dim / 8) * kTokens;
+  return dim3(unsigned((n_tokens + per - 1) / per), unsigned(c.n_kv_heads));
 }
 
 }  // namespace
@@ -208,6 +294,11 @@ dim3 token_grid(const fq_kv_cache& c, int64_t n_tokens) {
 }  // namespace fqk
 
 namespace fqi {
+
+namespace {
+// Outputs larger than this go past the caches.
+constexpr int64_t kStreamBytes = int64_t(32) << 20;
+}  // namespace
 
 int launch_kv_write(const fq_kv_cache& c, const uint16_t* K, const uint16_t* V,
                     int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
@@ -224,13 +315,17 @@ int launch_kv_write(const fq_kv_cache& c, const uint16_t* K, const uint16_t* V,
 int launch_kv_read(const fq_kv_cache& c, const int64_t* slots, int64_t n_tokens, void* K, void* V,
                    bool f32, void* stream) {
   const fqk::CacheArgs a = fqk::cache_args(c);
+  const bool past = 2 * n_tokens * c.n_kv_heads * c.head_dim * (f32 ? 4 : 2) > kStreamBytes;
   fqk::by_kind(c, [&](auto kind, auto dim) {
-    if (f32)
-      hipLaunchKernelGGL((fqk::kv_read_kernel<kind.value, dim.value, true>), fqk::token_grid(c, n_tokens), dim3(256),
-                         0, static_cast<hipStream_t>(stream), a, slots, int(n_tokens), K, V);
-    else
-      hipLaunchKernelGGL((fqk::kv_read_kernel<kind.value, dim.value, false>), fqk::token_grid(c, n_tokens), dim3(256),
-                         0, static_cast<hipStream_t>(stream), a, slots, int(n_tokens), K, V);
+    auto go = [&](auto wide, auto streamed) {
+      hipLaunchKernelGGL((fqk::kv_read_kernel<kind.value, dim.value, wide.value, streamed.value>),
+                         fqk::token_grid(c, n_tokens), dim3(256), 0, static_cast<hipStream_t>(stream), a, slots,
+                         int(n_tokens), K, V);
+    };
+    if (f32 && past) go(std::true_type{}, std::true_type{});
+    else if (f32) go(std::true_type{}, std::false_type{});
+    else if (past) go(std::false_type{}, std::true_type{});
+    else go(std::false_type{}, std::false_type{});
   });
   return int(hipGetLastError());
 }

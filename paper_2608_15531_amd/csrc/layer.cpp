@@ -15,6 +15,10 @@ bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p
 
 bool is_stride(int64_t s, int64_t unit) { return s >= 0 && s % unit == 0; }
 
+// The stride of a dimension of n: that of one place alone is never used, and callers
+// keep any number there.
+int64_t used(int64_t stride, int64_t n) { return n > 1 ? stride : 0; }
+
 // Sizes, kind and strides: all that needs no pointer.
 fq_status check_cache_sizes(const fq_kv_cache* c) {
   if (!c) return FQ_ERR_NULL;
@@ -23,14 +27,16 @@ fq_status check_cache_sizes(const fq_kv_cache* c) {
   if (c->head_dim != 64 && c->head_dim != 128) return FQ_ERR_UNSUPPORTED;
   if (c->page_size % fqi::kKvBlock != 0 || c->page_size > 65536) return FQ_ERR_UNSUPPORTED;
   if (c->n_pages > INT32_MAX || c->n_kv_heads > 65535) return FQ_ERR_UNSUPPORTED;
-  if (c->page_stride < 0 || c->head_stride < 0 || c->token_stride < 0) return FQ_ERR_SHAPE;
+  const int64_t page_stride = used(c->page_stride, c->n_pages), head_stride = used(c->head_stride, c->n_kv_heads);
+  if (page_stride < 0 || head_stride < 0 || c->token_stride < 0) return FQ_ERR_SHAPE;
   // byte offsets inside a 16-token block are 32 bits wide in the kernels
   if (c->token_stride > INT32_MAX / 32) return FQ_ERR_UNSUPPORTED;
-  if (!is_stride(c->page_stride, 16) || !is_stride(c->head_stride, 16) || !is_stride(c->token_stride, 16))
-    return FQ_ERR_ALIGN;
+  if (page_stride % 16 != 0 || head_stride % 16 != 0 || c->token_stride % 16 != 0) return FQ_ERR_ALIGN;
   if (c->kind != FQ_KV_BF16) {
-    if (c->meta_page_stride < 0 || c->meta_head_stride < 0) return FQ_ERR_SHAPE;
-    if (!is_stride(c->meta_page_stride, 4) || !is_stride(c->meta_head_stride, 4)) return FQ_ERR_ALIGN;
+    const int64_t meta_page = used(c->meta_page_stride, c->n_pages);
+    const int64_t meta_head = used(c->meta_head_stride, c->n_kv_heads);
+    if (meta_page < 0 || meta_head < 0) return FQ_ERR_SHAPE;
+    if (meta_page % 4 != 0 || meta_head % 4 != 0) return FQ_ERR_ALIGN;
   }
   return FQ_OK;
 }
@@ -57,11 +63,12 @@ fq_status check_attention(const fq_attention* a, const fq_kv_cache* c) {
   if (a->n_heads % c->n_kv_heads != 0) return FQ_ERR_SHAPE;
   if (int64_t(a->table_cols) * c->page_size < a->max_kv) return FQ_ERR_SHAPE;
   if (!std::isfinite(a->scale)) return FQ_ERR_SHAPE;
-  if (a->q_token_stride < 0 || a->q_head_stride < 0 || a->o_token_stride < 0 || a->o_head_stride < 0)
-    return FQ_ERR_SHAPE;
-  if (!is_stride(a->q_token_stride, 8) || !is_stride(a->q_head_stride, 8) ||
-      !is_stride(a->o_token_stride, 8) || !is_stride(a->o_head_stride, 8))
-    return FQ_ERR_ALIGN;
+  const int64_t strides[4] = {used(a->q_token_stride, a->total_q), used(a->q_head_stride, a->n_heads),
+                              used(a->o_token_stride, a->total_q), used(a->o_head_stride, a->n_heads)};
+  for (int64_t s : strides)
+    if (s < 0) return FQ_ERR_SHAPE;
+  for (int64_t s : strides)
+    if (s % 8 != 0) return FQ_ERR_ALIGN;
   // key numbers below 2^28 (the kernels' division by the page size), positions 32 bits wide
   if (a->max_kv > (1 << 28) || a->max_q > (1 << 28)) return FQ_ERR_UNSUPPORTED;
   return FQ_OK;
@@ -79,8 +86,12 @@ fq_status fq_kv_cache_write(const fq_kv_cache* cache, const uint16_t* K, const u
                             int64_t n_tokens, void* stream) {
   const fq_status st = check_cache(cache);
   if (st != FQ_OK) return st;
-  if (n_tokens < 0 || k_token_stride < 0 || k_head_stride < 0 || v_token_stride < 0 || v_head_stride < 0)
-    return FQ_ERR_SHAPE;
+  if (n_tokens < 0) return FQ_ERR_SHAPE;
+  k_token_stride = used(k_token_stride, n_tokens);
+  v_token_stride = used(v_token_stride, n_tokens);
+  k_head_stride = used(k_head_stride, cache->n_kv_heads);
+  v_head_stride = used(v_head_stride, cache->n_kv_heads);
+  if (k_token_stride < 0 || k_head_stride < 0 || v_token_stride < 0 || v_head_stride < 0) return FQ_ERR_SHAPE;
   if (n_tokens == 0) return FQ_OK;
   if (!K || !V || !slots) return FQ_ERR_NULL;
   if (!is_stride(k_token_stride, 8) || !is_stride(k_head_stride, 8) || !is_stride(v_token_stride, 8) ||

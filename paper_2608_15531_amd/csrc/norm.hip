@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include "device.hpp"
+#include "lanes.hpp"
 #include "layer.hpp"
 
 namespace fqk {
@@ -96,8 +97,7 @@ __device__ __forceinline__ void store8(float* p, int n, const float v[8]) {
 // float per wave; a second sum of the same row uses another one.
 template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float* part) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m);
+  v = over_lanes<64>(v, Add{});
   if constexpr (TPR > 64) {
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
