@@ -134,12 +134,16 @@ struct VRows {
 
 constexpr int kWaves = 4;
 
-// LDS: the waves' sums [kWaves][16][D + 4], then their maxima and row sums.
+constexpr int kMaxSplit = 128;   // ranges
+
+// LDS: the waves' sums [kWaves][16][D + 4], then their maxima and row sums; for the join of
+// the ranges their maxima and row sums [2][16][kMaxSplit] and 16 rows of sums instead.
 template <int D>
-constexpr size_t kAttnLds = (size_t(kWaves) * 16 * (D + 4) + 2 * kWaves * 16) * 4;
+constexpr size_t kAttnLds = std::max((size_t(kWaves) * 16 * (D + 4) + 2 * kWaves * 16) * 4,
+                                     (size_t(2) * 16 * kMaxSplit + 16 * D) * 4);
 
 template <int KIND, int D>
-__global__ void __launch_bounds__(64 * kWaves) attn_rows_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(64 * kWaves, 4) attn_rows_kernel(AttnArgs a) {
   constexpr int STEPS = D / 32, CB = D / 16;
   extern __shared__ __attribute__((aligned(16))) float lds[];
   __shared__ uint32_t last_flag;
@@ -363,27 +367,73 @@ __global__ void __launch_bounds__(64 * kWaves) attn_rows_kernel(AttnArgs a) {
     __syncthreads();
     if (!last_flag) return;
     if (tid == 0) __hip_atomic_store(a.counters + item, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (row >= it.rows) return;
-    // the last to arrive adds the ranges in their order
-    mx = kNegInf;
+    // The last to arrive adds the ranges.  A trip to memory costs more than a range's sums
+    // are worth, so few trips: the 16-thread groups that have no row of their own share the
+    // ranges with those that do, all maxima are read at once and the sums eight at a time.
+    // Every sum has a fixed order.
+    const int p2 = it.rows <= 1 ? 1 : it.rows <= 2 ? 2 : it.rows <= 4 ? 4 : it.rows <= 8 ? 8 : 16;
+    const int groups = 16 / p2, g = (tid >> 4) / p2, grow = (tid >> 4) % p2, i16 = tid & 15;
+    const uint32_t row_at = uint32_t(min(grow, it.rows - 1)) * (D + 4) * 4u;
+    float* weight = lds + grow * kMaxSplit;
+    float* sums = lds + (16 + grow) * kMaxSplit;
+    float* shared_o = lds + 2 * 16 * kMaxSplit;   // [groups][p2][D]
+    {
+      f32x4_t ms[kMaxSplit / 16];
+#pragma unroll
+      for (int j = 0; j < kMaxSplit / 16; ++j) {
+        const int s2 = (j * groups + g) * 16 + i16;
+        if (j * groups * 16 < it.n_parts)
+          ms[j] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
+              prs, int(uint32_t(min(s2, it.n_parts - 1)) * part_words * 4u + row_at + D * 4u), 0, kSc1));
+      }
+#pragma unroll
+      for (int j = 0; j < kMaxSplit / 16; ++j) {
+        const int s2 = (j * groups + g) * 16 + i16;
+        if (s2 < it.n_parts) {
+          weight[s2] = ms[j][0];
+          sums[s2] = ms[j][1];
+        }
+      }
+    }
+    __syncthreads();
+    float top = kNegInf;
+    for (int s2 = i16; s2 < it.n_parts; s2 += 16) top = fmaxf(top, weight[s2]);
+    mx = over_lanes<16>(top, Max{});
+    const float b2 = mx == kNegInf ? 0.f : mx;
     sum = 0.f;
+    for (int s2 = i16; s2 < it.n_parts; s2 += 16) sum = fmaf(__builtin_amdgcn_exp2f(weight[s2] - b2), sums[s2], sum);
+    sum = over_lanes<16>(sum, Add{});
 #pragma unroll
     for (int c = 0; c < CB; ++c) o[c] = 0.f;
-    for (int s2 = 0; s2 < it.n_parts; ++s2) {
-      const uint32_t at = (uint32_t(s2) * part_words + uint32_t(row) * (D + 4)) * 4u;
-      const f32x4_t ms = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(prs, int(at + D * 4u), 0, kSc1));
-      const float m2 = fmaxf(mx, ms[0]);
-      const float b2 = m2 == kNegInf ? 0.f : m2;
-      const float f0 = __builtin_amdgcn_exp2f(mx - b2), f1 = __builtin_amdgcn_exp2f(ms[0] - b2);
-      mx = m2;
-      sum = fmaf(sum, f0, f1 * ms[1]);
+    for (int s0 = g; s0 < it.n_parts; s0 += 8 * groups) {
+      u32x4_t v[8][CB / 4];
 #pragma unroll
-      for (int c = 0; c < CB; c += 4) {
-        const f32x4_t v = __builtin_bit_cast(
-            f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(prs, int(at + (ch + c) * 4u), 0, kSc1));
+      for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[c + i] = fmaf(o[c + i], f0, f1 * v[i]);
+        for (int c = 0; c < CB / 4; ++c)   // in range; surplus loads unused
+          v[j][c] = __builtin_amdgcn_raw_buffer_load_b128(
+              prs, int(uint32_t(min(s0 + j * groups, it.n_parts - 1)) * part_words * 4u + row_at + (ch + 4 * c) * 4u), 0, kSc1);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (s0 + j * groups >= it.n_parts) break;
+        const float f = __builtin_amdgcn_exp2f(weight[s0 + j * groups] - b2);
+#pragma unroll
+        for (int c = 0; c < CB / 4; ++c) {
+          const f32x4_t x = __builtin_bit_cast(f32x4_t, v[j][c]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[4 * c + e] = fmaf(f, x[e], o[4 * c + e]);
+        }
       }
+    }
+    if (groups > 1) {
+#pragma unroll
+      for (int c = 0; c < CB; c += 4)
+        *reinterpret_cast<f32x4_t*>(shared_o + (g * p2 + grow) * D + ch + c) = f32x4_t{o[c], o[c + 1], o[c + 2], o[c + 3]};
+      __syncthreads();
+      if (g > 0 || grow >= it.rows) return;
+      for (int g2 = 1; g2 < groups; ++g2)
+#pragma unroll
+        for (int c = 0; c < CB; ++c) o[c] += shared_o[(g2 * p2 + grow) * D + ch + c];
     }
   }
   if (row >= it.rows) return;
@@ -409,8 +459,12 @@ namespace fqi {
 
 namespace {
 
-constexpr int kTargetWorkgroups = 1024;   // four to a CU
-constexpr int kMinSplitTiles = 8;         // 256 keys a range: two tiles a wave
+// The kernel for few rows splits the keys until there are two workgroups to a CU, into
+// ranges of 128 keys (a tile a wave) at least, and always into ranges of 1024 keys at most,
+// which evens out sequences of different lengths.
+constexpr int kTargetWorkgroups = 512;
+constexpr int kMinSplitTiles = 4;
+constexpr int kMaxSplitTiles = 32;
 constexpr int kTilesMinRows = 32;         // more rows: the kernel for many rows
 constexpr int kTargetTileWorkgroups = 512;
 constexpr int kMinSplitBigTiles = 4;
@@ -441,6 +495,8 @@ bool plan_attention(const fq_attention& a, const fq_kv_cache& c, AttnPlan* pl) {
   int64_t split = 1;
   if (items <= kMaxStrips && items < target)
     split = std::max<int64_t>(1, std::min(ceil_div(target, items), tiles / shortest));
+  if (pl->kernel == FQ_ATTN_ROWS && items <= kMaxStrips)
+    split = std::min<int64_t>(std::max(split, ceil_div(tiles, kMaxSplitTiles)), fqk::kMaxSplit);
   pl->split_tiles = int(ceil_div(tiles, split));
   pl->split = int(ceil_div(tiles, pl->split_tiles));
   if (pl->split * row_blocks * c.n_kv_heads > INT32_MAX) return false;
