@@ -81,10 +81,6 @@ struct KRow {
   }
 };
 
-// The offset that operand() adds to the codes.
-template <int KIND>
-constexpr float kKvOffset = KIND == FQ_KV_INT4 ? kCodeOffset : 0.f;
-
 // Eight V rows' share of a lane: D / 16 channels from (lane & 15) * D / 16 on.
 template <int KIND, int D>
 struct VRows {
@@ -158,13 +154,19 @@ __global__ void __launch_bounds__(64 * kWaves, 4) attn_rows_kernel(AttnArgs a) {
   if (!it.set<16, kKvTile>(a)) return;
   Row mine;
   mine.set(a, it, r16);
+  // softmax in powers of two of |scale|; a negative scale changes the sign of q, 0 makes it 0
+  const uint32_t q_sign = a.scale_log2 < 0.f ? 0x80008000u : 0u;
+  const float c2 = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
+  const float grow = 8.f / c2;
+  const bool use_q = mine.in && a.scale_log2 != 0.f;
   const uint16_t* qp = a.Q + (it.t0 + mine.token) * a.q_token + mine.head * a.q_head;
   bf16x8_t qv[STEPS];
   float q_sum = 0.f;
 #pragma unroll
   for (int st = 0; st < STEPS; ++st) {
     uint4 w{0, 0, 0, 0};
-    if (mine.in) w = *reinterpret_cast<const uint4*>(qp + q_channel<KIND, D>(st, q));
+    if (use_q) w = *reinterpret_cast<const uint4*>(qp + q_channel<KIND, D>(st, q));
+    w = uint4{w.x ^ q_sign, w.y ^ q_sign, w.z ^ q_sign, w.w ^ q_sign};
     if constexpr (KIND != FQ_KV_BF16) {
       const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -175,6 +177,9 @@ __global__ void __launch_bounds__(64 * kWaves, 4) attn_rows_kernel(AttnArgs a) {
     qv[st] = __builtin_bit_cast(bf16x8_t, w);
   }
   if constexpr (KIND != FQ_KV_BF16) q_sum = row_add(q_sum);
+  // the offset of the codes is taken off where the products of K start from
+  const float from = KIND == FQ_KV_INT4 ? -kCodeOffset * q_sum : 0.f;
+  const f32x4_t d0{from, from, from, from};
 
   f32x4_t acc[CB];
 #pragma unroll
@@ -208,76 +213,65 @@ __global__ void __launch_bounds__(64 * kWaves, 4) attn_rows_kernel(AttnArgs a) {
         vm[h] = *reinterpret_cast<const uint4*>(vmh + at.page * a.meta_page_stride + at.token + 4 * q);
       }
     }
-    // scores, in powers of two
+    // scores
     float s[8];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      f32x4_t d{0.f, 0.f, 0.f, 0.f};
+      f32x4_t d = d0;
 #pragma unroll
       for (int st = 0; st < STEPS; ++st) d = mfma16(kr[h].operand(st), qv[st], d);
       const uint32_t kmw[4] = {km[h].x, km[h].y, km[h].z, km[h].w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if constexpr (KIND == FQ_KV_BF16) {
-          s[4 * h + j] = d[j] * a.scale_log2;
-        } else {
-          const float z = __builtin_bit_cast(float, kmw[j] & 0xFFFF0000u) + kKvOffset<KIND>;
-          s[4 * h + j] = fmaf(-z, q_sum, d[j]) * (bf16_bits_to_f32(kmw[j]) * a.scale_log2);
-        }
+        if constexpr (KIND == FQ_KV_BF16) s[4 * h + j] = d[j];
+        else s[4 * h + j] = fmaf(-__builtin_bit_cast(float, kmw[j] & 0xFFFF0000u), q_sum, d[j]) * bf16_bits_to_f32(kmw[j]);
       }
     }
-    // the mask, where the tile is not seen whole by every row
+    // the mask, where the tile is not seen whole by every row; a key that is not seen counts
+    // nothing, whatever its scale and zero-point
     const bool whole = it.whole<kKvTile>(a, key0);
-    uint32_t seen = 0xFFu;
+    uint32_t vmw[8] = {vm[0].x, vm[0].y, vm[0].z, vm[0].w, vm[1].x, vm[1].y, vm[1].z, vm[1].w};
     if (!whole) {
-      seen = 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int key = key0 + (j >> 2) * kKvBlock + 4 * q + (j & 3);
-        const bool see = mine.sees(a, key);
-        seen |= uint32_t(see) << j;
+        const bool see = mine.sees(a, key0 + (j >> 2) * kKvBlock + 4 * q + (j & 3));
         s[j] = see ? s[j] : kNegInf;
+        if constexpr (KIND != FQ_KV_BF16) vmw[j] = see ? vmw[j] : 0u;
       }
     }
     float top = s[0];
 #pragma unroll
     for (int j = 1; j < 8; ++j) top = fmaxf(top, s[j]);
     top = row_max(top);
-    const float m_new = fmaxf(m, top);
-    const float base = m_new == kNegInf ? 0.f : m_new;
-    const float shrink = __builtin_amdgcn_exp2f(m - base);
-    m = m_new;
-    float p[8];
-    float sum = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      p[j] = __builtin_amdgcn_exp2f(s[j] - base);
-      sum += p[j];
-    }
-    l = fmaf(l, shrink, sum);
-    u32x4_t pw;
-    if constexpr (KIND == FQ_KV_BF16) {
-#pragma unroll
-      for (int i2 = 0; i2 < 4; ++i2) pw[i2] = pk_bf16(p[2 * i2], p[2 * i2 + 1]);
-    } else {
-      const uint32_t vmw[8] = {vm[0].x, vm[0].y, vm[0].z, vm[0].w, vm[1].x, vm[1].y, vm[1].z, vm[1].w};
+    // the sums move to a new maximum only when some row's has grown by more than 2^8: until
+    // then its weights are up to 2^8, which fp32 sums and bf16 weights hold as well
+    if (__any(top > m + grow)) {
+      const float m_new = fmaxf(m, top);
+      const float shrink = __builtin_amdgcn_exp2f((m - (m_new == kNegInf ? 0.f : m_new)) * c2);
+      m = m_new;
+      l *= shrink;
       corr *= shrink;
 #pragma unroll
-      for (int i2 = 0; i2 < 4; ++i2) {
-        const uint32_t m0 = vmw[2 * i2], m1 = vmw[2 * i2 + 1];
-        // a key that is not seen counts nothing, whatever its scale
-        const float a0 = (seen >> (2 * i2)) & 1u ? p[2 * i2] * bf16_bits_to_f32(m0) : 0.f;
-        const float a1 = (seen >> (2 * i2 + 1)) & 1u ? p[2 * i2 + 1] * bf16_bits_to_f32(m1) : 0.f;
-        pw[i2] = pk_bf16(a0, a1);
-        const float b0 = bf16_bits_to_f32(pw[i2]), b1 = __builtin_bit_cast(float, pw[i2] & 0xFFFF0000u);
-        const float z0 = (seen >> (2 * i2)) & 1u ? __builtin_bit_cast(float, m0 & 0xFFFF0000u) : 0.f;
-        const float z1 = (seen >> (2 * i2 + 1)) & 1u ? __builtin_bit_cast(float, m1 & 0xFFFF0000u) : 0.f;
-        corr = fmaf(b0, z0 + kKvOffset<KIND>, corr);
-        corr = fmaf(b1, z1 + kKvOffset<KIND>, corr);
+      for (int c = 0; c < CB; ++c) acc[c] *= shrink;
+    }
+    const float base = m == kNegInf ? 0.f : -m * c2;
+    float p[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], c2, base));
+      l += p[j];
+      if constexpr (KIND != FQ_KV_BF16) p[j] *= bf16_bits_to_f32(vmw[j]);
+    }
+    u32x4_t pw;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      pw[e] = pk_bf16(p[2 * e], p[2 * e + 1]);
+      if constexpr (KIND != FQ_KV_BF16) {
+        const uint32_t w = pw[e];
+        corr = dot2_bf16(w, __builtin_amdgcn_perm(vmw[2 * e + 1], vmw[2 * e], 0x07060302u), corr);
+        if constexpr (KIND == FQ_KV_INT4) corr = dot2_bf16(w, 0x43004300u, corr);   // the offset 128
       }
     }
-#pragma unroll
-    for (int c = 0; c < CB; ++c) acc[c] *= shrink;
     if constexpr (KIND == FQ_KV_BF16) {
       if (!whole) {
         bool any = false;
@@ -308,6 +302,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) attn_rows_kernel(AttnArgs a) {
   }
 
   // join the waves: lane (r16, q) has channels (4 q + i) CB + c of row r16
+  m *= c2;
   l = row_add(l);
   if constexpr (KIND != FQ_KV_BF16) corr = row_add(corr);
   {
