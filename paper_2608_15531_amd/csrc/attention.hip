@@ -455,11 +455,11 @@ namespace fqi {
 namespace {
 
 // The kernel for few rows splits the keys until there are two workgroups to a CU, into
-// ranges of 128 keys (a tile a wave) at least, and always into ranges of 1024 keys at most,
-// which evens out sequences of different lengths.
+// ranges of 128 keys (a tile a wave) at least.  Beyond that it makes eight ranges of the
+// longest sequence, of 768 to 4096 keys, which evens out sequences of different lengths.
 constexpr int kTargetWorkgroups = 512;
 constexpr int kMinSplitTiles = 4;
-constexpr int kMaxSplitTiles = 32;
+constexpr int kEvenRanges = 8, kEvenMinTiles = 24, kEvenMaxTiles = 128;
 constexpr int kTilesMinRows = 32;         // more rows: the kernel for many rows
 constexpr int kTargetTileWorkgroups = 512;
 constexpr int kMinSplitBigTiles = 4;
@@ -491,7 +491,9 @@ bool plan_attention(const fq_attention& a, const fq_kv_cache& c, AttnPlan* pl) {
   if (items <= kMaxStrips && items < target)
     split = std::max<int64_t>(1, std::min(ceil_div(target, items), tiles / shortest));
   if (pl->kernel == FQ_ATTN_ROWS && items <= kMaxStrips)
-    split = std::min<int64_t>(std::max(split, ceil_div(tiles, kMaxSplitTiles)), fqk::kMaxSplit);
+    split = std::min<int64_t>(
+        std::max(split, ceil_div(tiles, std::clamp<int64_t>(tiles / kEvenRanges, kEvenMinTiles, kEvenMaxTiles))),
+        fqk::kMaxSplit);
   pl->split_tiles = int(ceil_div(tiles, split));
   pl->split = int(ceil_div(tiles, pl->split_tiles));
   if (pl->split * row_blocks * c.n_kv_heads > INT32_MAX) return false;

@@ -103,7 +103,7 @@ __device__ __forceinline__ TileRange tile_range(int p_lo, int p_hi, int window, 
 struct Item {
   int head, seq, rb, part, n_parts;
   int64_t t0;          // first new token of the sequence
-  int64_t row0;        // first row of the block
+  uint32_t row0;       // first row of the block (the plan keeps rows below 2^31)
   int rows;
   int p0;              // position of the sequence's first new token
   int tok_hi;          // the block's last token
@@ -123,12 +123,12 @@ struct Item {
     const int64_t t1 = min(max(int64_t(a.cu_q[seq + 1]), t0), a.total_q);
     const int q_all = int(t1 - t0);               // before the bound: positions count from the end
     const int kv_len = max(a.kv_lens[seq], 0);
-    const int64_t n_rows = int64_t(min(q_all, a.max_q)) * a.group;
-    row0 = int64_t(rb) * ROWS;
+    const uint32_t group = uint32_t(a.group), n_rows = uint32_t(min(q_all, a.max_q)) * group;
+    row0 = uint32_t(rb) * ROWS;
     if (row0 >= n_rows) return false;
-    rows = int(min(n_rows - row0, int64_t(ROWS)));
-    const int tok_lo = int(row0 / a.group);
-    tok_hi = int((row0 + rows - 1) / a.group);
+    rows = int(min(n_rows - row0, uint32_t(ROWS)));
+    const int tok_lo = int(row0 / group);
+    tok_hi = int((row0 + rows - 1) / group);
     p0 = kv_len - q_all;
     kv_seen = min(kv_len, a.max_kv);
     p_lo = min(p0 + tok_lo, kv_seen - 1);
@@ -155,9 +155,9 @@ struct Row {
   int win_lo;    // first key of its window
   __device__ __forceinline__ void set(const AttnArgs& a, const Item& it, int r) {
     in = r < it.rows;
-    const int64_t row = it.row0 + min(r, it.rows - 1);
-    token = int(row / a.group);
-    head = it.head * a.group + int(row - int64_t(token) * a.group);
+    const uint32_t row = it.row0 + uint32_t(min(r, it.rows - 1)), group = uint32_t(a.group);
+    token = int(row / group);
+    head = it.head * a.group + int(row - uint32_t(token) * group);
     pos = in ? min(it.p0 + token, it.kv_seen - 1) : -1;
     win_lo = a.window > 0 ? it.p0 + token - a.window + 1 : INT_MIN;
   }

@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
   mine.set(a, it, wave * 32 + r32);
   // what the rows of this wave see, for leaving tiles out and for the mask
   const int w_lo = min(wave * 32, it.rows - 1), w_hi = min(wave * 32 + 31, it.rows - 1);
-  const int wt_lo = it.p0 + int((it.row0 + w_lo) / a.group), wt_hi = it.p0 + int((it.row0 + w_hi) / a.group);
+  const int wt_lo = it.p0 + int((it.row0 + w_lo) / uint32_t(a.group)), wt_hi = it.p0 + int((it.row0 + w_hi) / uint32_t(a.group));
   const int wp_lo = min(wt_lo, it.kv_seen - 1);
   const int wp_hi = wave * 32 < it.rows ? min(wt_hi, it.kv_seen - 1) : -1;
 
