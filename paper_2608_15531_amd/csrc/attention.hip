@@ -461,8 +461,11 @@ constexpr int kTargetWorkgroups = 512;
 constexpr int kMinSplitTiles = 4;
 constexpr int kEvenRanges = 8, kEvenMinTiles = 24, kEvenMaxTiles = 128;
 constexpr int kTilesMinRows = 32;         // more rows: the kernel for many rows
-constexpr int kTargetTileWorkgroups = 512;
-constexpr int kMinSplitBigTiles = 4;
+// The kernel for many rows has two workgroups to a CU; it splits the keys where that makes
+// rounds * (tiles of a range + kRangeCost) smaller, a range's start and its part in the join
+// being worth so many tiles.
+constexpr int kTileSlots = 512;
+constexpr int kRangeCost = 4;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -484,16 +487,20 @@ bool plan_attention(const fq_attention& a, const fq_kv_cache& c, AttnPlan* pl) {
   if (a.window > 0)
     tiles = std::min<int64_t>(tiles, ceil_div(a.window + ceil_div(pl->rows, group), pl->tile) + 2 +
                                          ceil_div(a.sinks, pl->tile));
-  // enough ranges to fill the GPU, none of them short; every item has a counter
-  const int64_t target = pl->kernel == FQ_ATTN_TILES ? kTargetTileWorkgroups : kTargetWorkgroups;
-  const int64_t shortest = pl->kernel == FQ_ATTN_TILES ? kMinSplitBigTiles : kMinSplitTiles;
   int64_t split = 1;
-  if (items <= kMaxStrips && items < target)
-    split = std::max<int64_t>(1, std::min(ceil_div(target, items), tiles / shortest));
-  if (pl->kernel == FQ_ATTN_ROWS && items <= kMaxStrips)
-    split = std::min<int64_t>(
-        std::max(split, ceil_div(tiles, std::clamp<int64_t>(tiles / kEvenRanges, kEvenMinTiles, kEvenMaxTiles))),
-        fqk::kMaxSplit);
+  if (items <= kMaxStrips) {   // every item has a counter
+    if (pl->kernel == FQ_ATTN_TILES) {
+      const auto cost = [&](int64_t n) { return ceil_div(items * n, kTileSlots) * (ceil_div(tiles, n) + kRangeCost); };
+      for (int64_t n = 2; n <= std::min<int64_t>(tiles / 2, 64); ++n)
+        if (cost(n) < cost(split)) split = n;
+    } else {
+      if (items < kTargetWorkgroups)
+        split = std::max<int64_t>(1, std::min(ceil_div(kTargetWorkgroups, items), tiles / kMinSplitTiles));
+      split = std::min<int64_t>(
+          std::max(split, ceil_div(tiles, std::clamp<int64_t>(tiles / kEvenRanges, kEvenMinTiles, kEvenMaxTiles))),
+          fqk::kMaxSplit);
+    }
+  }
   pl->split_tiles = int(ceil_div(tiles, split));
   pl->split = int(ceil_div(tiles, pl->split_tiles));
   if (pl->split * row_blocks * c.n_kv_heads > INT32_MAX) return false;

@@ -77,6 +77,13 @@ struct Share {
   __device__ static __forceinline__ Places places(const AttnArgs& a, const int32_t* table, int key0, int kv_seen,
                                                   int wave) {
     Places p;
+    if (a.page_blocks % (kTile / kKvBlock) == 0) {   // one look-up where pages hold whole tiles
+      const BlockPlace first = block_place(a, table, key0);
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+        p.at[i] = BlockPlace{first.page, first.token + uint32_t((i * 256 + wave * 64) / PPR / kKvBlock * kKvBlock)};
+      return p;
+    }
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int key = key0 + (i * 256 + wave * 64) / PPR / kKvBlock * kKvBlock;
@@ -328,12 +335,17 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
                          (a.window == 0 || key0 > wt_hi - a.window || key0 + kTile <= a.sinks);
       uint32_t seen = ~0u;   // bit 16 kb + j
       if (!whole) {
+        // bounds of the keys' constant places in the tile, so that the comparisons take
+        // constants and no register for each key
+        const int from = key0 + 4 * h, last = mine.pos - from, window = max(mine.win_lo, -(1 << 30)) - from,
+                  sinks = a.sinks - from;
         seen = 0u;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
-            const bool see = mine.sees(a, key0 + kb * 32 + 8 * (j / 4) + 4 * h + j % 4);
+            const int c = kb * 32 + 8 * (j / 4) + j % 4;
+            const bool see = c <= last && (c >= window || c < sinks);
             s[kb][j] = see ? s[kb][j] : kNegInf;
             seen |= see ? 1u << (16 * kb + j) : 0u;
           }
