@@ -460,12 +460,21 @@ namespace {
 constexpr int kTargetWorkgroups = 512;
 constexpr int kMinSplitTiles = 4;
 constexpr int kEvenRanges = 8, kEvenMinTiles = 24, kEvenMaxTiles = 128;
-constexpr int kTilesMinRows = 32;         // more rows: the kernel for many rows
+// The kernel for few rows reads the keys once for each block of 16 rows, the one for many
+// once for 128, at a longer start and with a second kernel for the join.  By measurement
+// (us, few / many), with what the blocks of 16 rows read in all: 40 tokens of 4 heads a
+// group over 540 keys, bf16, 22 MB: 10 / 18; 16 over 8000, bf16, 131 MB: 23 / 31; 300 over
+// 600, bf16, 184 MB: 18 / 27; 10 over 2000, 16 sequences, 8 bits, 204 MB: 31 / 40; but 16
+// over 4000, 8 sequences, 8 bits, 271 MB: 44 / 41; 20 over 2000, 8 sequences, bf16, 331 MB:
+// 34 / 28.
+constexpr int64_t kFewRowsBytes = int64_t(224) << 20;
 // The kernel for many rows has two workgroups to a CU; it splits the keys where that makes
 // rounds * (tiles of a range + kRangeCost) smaller, a range's start and its part in the join
 // being worth so many tiles.
 constexpr int kTileSlots = 512;
 constexpr int kRangeCost = 4;
+// Partial results are kept small: 2048 ranges of 128 rows are 138 MB, 8192 of 16 rows 69.
+constexpr int kMostTileRanges = 2048, kMostRanges = 8192;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -474,7 +483,11 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool plan_attention(const fq_attention& a, const fq_kv_cache& c, AttnPlan* pl) {
   const int64_t group = a.n_heads / c.n_kv_heads;
   const int64_t rows = a.max_q * group;
-  pl->kernel = rows > kTilesMinRows ? FQ_ATTN_TILES : FQ_ATTN_ROWS;
+  const int64_t key_bytes = c.kind == FQ_KV_BF16 ? 4 * c.head_dim : c.kind == FQ_KV_INT8 ? 2 * c.head_dim + 8
+                                                                                        : c.head_dim + 8;
+  const int64_t seen_keys = a.window > 0 ? std::min<int64_t>(a.max_kv, int64_t(a.window) + a.sinks + a.max_q) : a.max_kv;
+  const bool few = rows <= 32 || ceil_div(rows, 16) * a.n_seqs * c.n_kv_heads <= kFewRowsBytes / (seen_keys * key_bytes);
+  pl->kernel = few ? FQ_ATTN_ROWS : FQ_ATTN_TILES;
   pl->rows = pl->kernel == FQ_ATTN_TILES ? kTilesRows : 16;
   pl->tile = pl->kernel == FQ_ATTN_TILES ? kTilesKeys : kKvTile;
   const int64_t row_blocks = ceil_div(rows, pl->rows);
@@ -491,14 +504,14 @@ bool plan_attention(const fq_attention& a, const fq_kv_cache& c, AttnPlan* pl) {
   if (items <= kMaxStrips) {   // every item has a counter
     if (pl->kernel == FQ_ATTN_TILES) {
       const auto cost = [&](int64_t n) { return ceil_div(items * n, kTileSlots) * (ceil_div(tiles, n) + kRangeCost); };
-      for (int64_t n = 2; n <= std::min<int64_t>(tiles / 2, 64); ++n)
+      for (int64_t n = 2; n <= std::min<int64_t>(tiles / 2, 64) && items * n <= kMostTileRanges; ++n)
         if (cost(n) < cost(split)) split = n;
     } else {
       if (items < kTargetWorkgroups)
         split = std::max<int64_t>(1, std::min(ceil_div(kTargetWorkgroups, items), tiles / kMinSplitTiles));
       split = std::min<int64_t>(
           std::max(split, ceil_div(tiles, std::clamp<int64_t>(tiles / kEvenRanges, kEvenMinTiles, kEvenMaxTiles))),
-          fqk::kMaxSplit);
+          std::min<int64_t>(fqk::kMaxSplit, std::max<int64_t>(1, kMostRanges / items)));
     }
   }
   pl->split_tiles = int(ceil_div(tiles, split));

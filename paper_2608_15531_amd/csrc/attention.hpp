@@ -112,13 +112,12 @@ struct Item {
   TileRange tr;
   int i_lo, i_hi;      // this range of the block's tiles
 
+  // The block's rows and tiles; false: the sequence has no such rows.
   template <int ROWS, int TILE>
-  __device__ __forceinline__ bool set(const AttnArgs& a) {
-    head = int(blockIdx.x) % a.n_kv_heads;
-    const int x = int(blockIdx.x) / a.n_kv_heads;
-    part = x % a.split;
-    rb = a.row_blocks - 1 - x / a.split;
-    seq = int(blockIdx.y);
+  __device__ __forceinline__ bool set_rows(const AttnArgs& a, int seq_, int rb_, int head_) {
+    seq = seq_;
+    rb = rb_;
+    head = head_;
     t0 = min(max(int64_t(a.cu_q[seq]), int64_t(0)), a.total_q);
     const int64_t t1 = min(max(int64_t(a.cu_q[seq + 1]), t0), a.total_q);
     const int q_all = int(t1 - t0);               // before the bound: positions count from the end
@@ -134,7 +133,20 @@ struct Item {
     p_lo = min(p0 + tok_lo, kv_seen - 1);
     p_hi = min(p0 + tok_hi, kv_seen - 1);
     tr = tile_range<TILE>(p_lo, p_hi, a.window, a.sinks);
-    n_parts = min(max(1, (tr.n + a.split_tiles - 1) / a.split_tiles), a.split);
+    return true;
+  }
+  // how many ranges its tiles fall into
+  __device__ __forceinline__ int parts(const AttnArgs& a) const {
+    return min(max(1, (tr.n + a.split_tiles - 1) / a.split_tiles), a.split);
+  }
+  // What this workgroup works on; false: nothing.
+  template <int ROWS, int TILE>
+  __device__ __forceinline__ bool set(const AttnArgs& a) {
+    const int x = int(blockIdx.x) / a.n_kv_heads;
+    part = x % a.split;
+    if (!set_rows<ROWS, TILE>(a, int(blockIdx.y), a.row_blocks - 1 - x / a.split, int(blockIdx.x) % a.n_kv_heads))
+      return false;
+    n_parts = parts(a);
     if (part >= n_parts) return false;
     i_lo = part * a.split_tiles;
     i_hi = min(i_lo + a.split_tiles, tr.n);

@@ -209,7 +209,7 @@ template <int KIND, int D>
 __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs a) {
   constexpr int STEPS = D / 16, DB = D / 32;
   extern __shared__ __attribute__((aligned(1024))) char tile_lds[];
-  __shared__ uint32_t last_flag, odd_flag;
+  __shared__ uint32_t odd_flag;
   const int tid = int(threadIdx.x), lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r32 = lane & 31, h = lane >> 5;
@@ -422,64 +422,20 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
   // lane (r32, h) has channels 32 c + 8 (i / 4) + 4 h + i % 4 of its row
   l = pair_add(l);
   if (it.n_parts > 1) {
-    // partial sums: [item][range][row][D + 4] floats, the last four: m c2, l
+    // partial sums for join_kernel: [item][range][row][D + 4] floats, the last four: m c2, l
     const int64_t item = (int64_t(it.seq) * a.n_kv_heads + it.head) * a.row_blocks + it.rb;
-    const uint32_t part_words = uint32_t(a.part_rows) * (D + 4);
-    const __amdgpu_buffer_rsrc_t prs =
-        make_rsrc(a.partials + item * a.split * part_words, uint32_t(a.split) * part_words * 4u);
-    const uint32_t row_at = uint32_t(wave * 32 + r32) * (D + 4) * 4u;
-    m *= c2;
-    if (mine.in) {
-      const uint32_t at = uint32_t(it.part) * part_words * 4u + row_at;
-#pragma unroll
-      for (int c = 0; c < DB; ++c)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          __builtin_amdgcn_raw_buffer_store_b128(
-              __builtin_bit_cast(u32x4_t, f32x4_t{acc[c][4 * g], acc[c][4 * g + 1], acc[c][4 * g + 2], acc[c][4 * g + 3]}),
-              prs, int(at + (32 * c + 8 * g + 4 * h) * 4u), 0, kSc1);
-      if (h == 0)
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, f32x4_t{m, l, 0.f, 0.f}), prs,
-                                               int(at + D * 4u), 0, kSc1);
-    }
-    __builtin_amdgcn_s_waitcnt(0);   // this thread's partial stores have completed
-    __syncthreads();
-    if (tid == 0) {
-      const uint32_t old = __hip_atomic_fetch_add(a.counters + item, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      last_flag = old == uint32_t(it.n_parts - 1);
-    }
-    __syncthreads();
-    if (!last_flag) return;
-    if (tid == 0) __hip_atomic_store(a.counters + item, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (!mine.in) return;
-    // the last to arrive adds the ranges in their order
-    m = kNegInf;
-    l = 0.f;
+    float* to = a.partials + ((item * a.split + it.part) * a.part_rows + wave * 32 + r32) * (D + 4);
 #pragma unroll
     for (int c = 0; c < DB; ++c)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
-    for (int part = 0; part < it.n_parts; ++part) {
-      const uint32_t at = uint32_t(part) * part_words * 4u + row_at;
-      const f32x4_t ms = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(prs, int(at + D * 4u), 0, kSc1));
-      const float m2 = fmaxf(m, ms[0]);
-      const float b2 = m2 == kNegInf ? 0.f : m2;
-      const float f0 = __builtin_amdgcn_exp2f(m - b2), f1 = __builtin_amdgcn_exp2f(ms[0] - b2);
-      m = m2;
-      l = fmaf(l, f0, f1 * ms[1]);
-#pragma unroll
-      for (int c = 0; c < DB; ++c)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const f32x4_t v = __builtin_bit_cast(
-              f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(prs, int(at + (32 * c + 8 * g + 4 * h) * 4u), 0, kSc1));
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[c][4 * g + j] = fmaf(acc[c][4 * g + j], f0, f1 * v[j]);
-        }
-    }
-  } else {
-    m *= c2;
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4_t*>(to + 32 * c + 8 * g + 4 * h) =
+            f32x4_t{acc[c][4 * g], acc[c][4 * g + 1], acc[c][4 * g + 2], acc[c][4 * g + 3]};
+    if (h == 0) *reinterpret_cast<f32x4_t*>(to + D) = f32x4_t{m * c2, l, 0.f, 0.f};
+    return;
   }
+  m *= c2;
   if (!mine.in) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   uint16_t* op = a.O + (it.t0 + mine.token) * a.o_token + mine.head * a.o_head;
@@ -496,9 +452,76 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
     a.lse[(it.t0 + mine.token) * a.n_heads + mine.head] = l == 0.f ? kNegInf : (m + __log2f(l)) * 0.69314718055994530942f;
 }
 
+// Joins the ranges of rows whose keys were split, in their order: D / 8 threads a row,
+// eight channels each.  (By the last workgroup of a block, as the kernel for few rows does,
+// the 128 rows of 32 ranges took 130 us of one CU.)
+template <int D>
+__global__ void __launch_bounds__(256) join_kernel(AttnArgs a) {
+  constexpr int T = D / 8, PER = 256 / T;   // threads a row, rows of a workgroup
+  constexpr int kBlocks = kRows / PER;      // workgroups of a block of rows
+  Item it;
+  const int x = int(blockIdx.x) / kBlocks, first = int(blockIdx.x) % kBlocks * PER;
+  const int head = x % a.n_kv_heads, rb = x / a.n_kv_heads;
+  if (!it.set_rows<kRows, kTile>(a, int(blockIdx.y), rb, head)) return;
+  const int n = it.parts(a);
+  const int r = first + int(threadIdx.x) / T, ch = int(threadIdx.x) % T * 8;
+  if (n <= 1 || r >= it.rows) return;
+  const int64_t item = (int64_t(it.seq) * a.n_kv_heads + it.head) * a.row_blocks + it.rb;
+  const int64_t step = int64_t(a.part_rows) * (D + 4);
+  const float* from = a.partials + item * a.split * step + int64_t(r) * (D + 4);
+  constexpr int U = 8;   // ranges read at a time
+  float m = kNegInf;
+  for (int p0 = 0; p0 < n; p0 += U) {
+    float t[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) t[u] = from[min(p0 + u, n - 1) * step + D];
+#pragma unroll
+    for (int u = 0; u < U; ++u) m = fmaxf(m, t[u]);
+  }
+  const float base = m == kNegInf ? 0.f : m;
+  float l = 0.f, o[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c) o[c] = 0.f;
+  for (int p0 = 0; p0 < n; p0 += U) {
+    f32x4_t v[U][2];
+    float2 ml[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {   // in range; surplus loads unused
+      const float* q = from + min(p0 + u, n - 1) * step;
+      v[u][0] = *reinterpret_cast<const f32x4_t*>(q + ch);
+      v[u][1] = *reinterpret_cast<const f32x4_t*>(q + ch + 4);
+      ml[u] = *reinterpret_cast<const float2*>(q + D);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float f = p0 + u < n ? __builtin_amdgcn_exp2f(ml[u].x - base) : 0.f;
+      l = fmaf(f, ml[u].y, l);
+      if (p0 + u < n) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          o[c] = fmaf(f, v[u][0][c], o[c]);
+          o[4 + c] = fmaf(f, v[u][1][c], o[4 + c]);
+        }
+      }
+    }
+  }
+  Row dst;
+  dst.set(a, it, r);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint32_t w[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) w[c] = l == 0.f ? 0u : pk_bf16(o[2 * c] * inv, o[2 * c + 1] * inv);
+  *reinterpret_cast<uint4*>(a.O + (it.t0 + dst.token) * a.o_token + dst.head * a.o_head + ch) = uint4{w[0], w[1], w[2], w[3]};
+  if (a.lse && ch == 0)
+    a.lse[(it.t0 + dst.token) * a.n_heads + dst.head] = l == 0.f ? kNegInf : (m + __log2f(l)) * 0.69314718055994530942f;
+}
+
 template <int KIND, int D>
 int launch_one(const AttnArgs& g, dim3 grid, hipStream_t s) {
   hipLaunchKernelGGL((attn_tiles_kernel<KIND, D>), grid, dim3(64 * kTileWaves), TileLds<D>::bytes, s, g);
+  if (g.split > 1)
+    hipLaunchKernelGGL((join_kernel<D>), dim3(grid.x / unsigned(g.split) * (kRows / (256 / (D / 8))), grid.y), dim3(256),
+                       0, s, g);
   return int(hipGetLastError());
 }
 

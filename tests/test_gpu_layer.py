@@ -218,7 +218,7 @@ class Step:
                     o, e, A, _ = L.attention_row(q[t, h], held[0][:, h // G], held[1][:, h // G], see, scale)
                     where = f"sequence {b} token {i} head {h}"
                     if see.any() and np.isfinite(e):
-                        big = (size[0][see, h // G] @ np.abs(q[t, h])).max() * scale
+                        big = (size[0][see, h // G] @ np.abs(q[t, h])).max() * abs(scale)
                         d = (self.D + 8) * 2.0 ** -24 * big
                         S_v = size[1][see, h // G].max(0) if self.kind != "bf16" else A
                         tol = B8 * 1.05 * np.abs(o) + (B8 * 1.05 + 2.5 * d) * A + 64 * 2.0 ** -24 * S_v + 1e-30
@@ -268,6 +268,91 @@ def test_attention(gpu_lib, name, kind, D):
     st.check(out, lse, window, sinks)
 
 
+def tiles_bounds(st, window=0, sinks=0, by_keys=False):
+    """Raises the step's bounds of the new tokens, or of the keys, until the kernel for many
+    rows is the one to run; returns the launch."""
+    q, kv, b = st.batch.max_q, st.batch.max_kv, st.batch
+    while True:
+        if by_keys:
+            kv *= 2
+        else:
+            q *= 2
+        cols = -(-kv // st.cache.page_size)
+        table = torch.full((len(st.q_lens), max(cols, st.table.shape[1])), -1, dtype=torch.int32)
+        table[:, :st.table.shape[1]] = st.table
+        st.batch = st.fq.PagedBatch(b.cu_q, b.kv_lens, table.cuda(), q, kv)
+        c = st.fq.fq_paged_attention_launch(st.hq, sum(st.q_lens), st.cache, st.batch, window=window, sinks=sinks)
+        if c["kernel"] == "tiles":
+            return c
+
+
+# (query heads, KV heads, page, new tokens, whole lengths, window, sinks)
+MANY = {
+    "chunk_on_a_prefix": (8, 2, 16, [90], [400], 0, 0),
+    "prompts_from_zero": (4, 1, 48, [64, 130, 1], [64, 130, 1], 0, 0),
+    "mixed_with_decoding": (8, 2, 64, [1, 120, 33], [500, 260, 33], 0, 0),
+    "window": (4, 2, 16, [130, 60], [300, 60], 50, 0),
+    "window_and_sinks": (8, 2, 32, [100, 1, 40], [420, 700, 41], 70, 5),
+    "window_of_one": (4, 2, 16, [70], [190], 1, 0),
+    "far_sinks": (4, 2, 16, [70], [500], 30, 129),
+    "more_tokens_than_keys": (8, 4, 16, [100, 70], [40, 0], 0, 0),
+    "mha": (2, 2, 16, [140], [300], 0, 0),
+    "group_of_three": (6, 2, 16, [45, 80], [100, 200], 0, 0),
+    "split_prefix": (4, 1, 16, [40], [3000], 0, 0),
+    "split_ragged": (8, 2, 16, [40, 1, 64], [2500, 900, 64], 0, 0),
+    "split_window": (4, 1, 64, [64], [2600], 1500, 70),
+}
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("name", list(MANY))
+def test_attention_many_rows(gpu_lib, name, kind, D):
+    """The kernel for many rows, and the join of its ranges."""
+    fq = gpu_lib
+    hq, hkv, page, q_lens, kv_lens, window, sinks = MANY[name]
+    st = Step(fq, kind, D, hq, hkv, page, q_lens, kv_lens, seed=3 * len(name) + D)
+    c = tiles_bounds(st, window, sinks, by_keys=name.startswith("split") and not window)
+    log(f"attention {name} {kind} D={D} {c}")
+    assert c["kernel"] == "tiles"
+    assert c["split"] > 1 or not name.startswith("split")
+    out, lse = fq.fq_paged_attention(st.q, st.cache, st.batch, window=window, sinks=sinks, return_lse=True)
+    torch.cuda.synchronize()
+    st.check(out, lse, window, sinks, rows=24)
+    again = fq.fq_paged_attention(st.q, st.cache, st.batch, window=window, sinks=sinks)
+    assert torch.equal(again, out)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("q_lens,kv_lens", [([2, 1], [300, 40]), ([60], [140])], ids=["rows", "tiles"])
+@pytest.mark.parametrize("scale", [-0.07, 0.0, 1e-30])
+def test_attention_scales(gpu_lib, scale, q_lens, kv_lens, kind):
+    """A scale that is negative, zero (the mean of the values) or next to it."""
+    fq = gpu_lib
+    st = Step(fq, kind, 128, 4, 2, 16, q_lens, kv_lens, seed=17)
+    if len(q_lens) == 1:
+        tiles_bounds(st)
+    log(f"attention scale {scale} {kind}")
+    out, lse = fq.fq_paged_attention(st.q, st.cache, st.batch, scale=scale, return_lse=True)
+    torch.cuda.synchronize()
+    st.check(out, lse, 0, 0, scale=scale, rows=12)
+
+
+def test_attention_kernel_by_rows_and_bytes(gpu_lib):
+    """Up to 32 rows the kernel for few; above by what the blocks of 16 rows read."""
+    fq = gpu_lib
+    small = make_cache(fq, "int4", 4, 16, 8, 128)
+    i32 = dict(dtype=torch.int32, device="cuda")
+
+    def kernel(max_q, max_kv, n_seqs):
+        b = fq.PagedBatch(torch.zeros(n_seqs + 1, **i32), torch.zeros(n_seqs, **i32), torch.zeros((n_seqs, 4096), **i32),
+                          max_q, max_kv)
+        return fq.fq_paged_attention_launch(32, 100, small, b)["kernel"]
+
+    assert kernel(8, 65536, 64) == "rows" and kernel(9, 65536, 64) == "tiles"
+    assert kernel(20, 8000, 1) == "rows" and kernel(20, 8000, 8) == "tiles"
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("q_lens,kv_lens", [([1, 1], [5000, 1234]), ([4], [9001]), ([100], [3000])],
                          ids=["decode", "draft", "chunk"])
@@ -303,8 +388,9 @@ def test_attention_orders_and_output_strides(gpu_lib, kind, order):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("tiles", [False, True], ids=["rows", "tiles"])
 @pytest.mark.parametrize("q", [4, 60], ids=["few", "many"])
-def test_attention_unseen_infinities_and_nan(gpu_lib, kind, q):
+def test_attention_unseen_infinities_and_nan(gpu_lib, kind, q, tiles):
     """Keys that some tokens see and others do not hold infinities and NaN in K and V:
     only the rows of the former may show them."""
     fq = gpu_lib
@@ -318,7 +404,9 @@ def test_attention_unseen_infinities_and_nan(gpu_lib, kind, q):
         v[bad, 1, 9] = float("nan")
 
     st = Step(fq, kind, D, 4, 2, 16, [q], [S], seed=3, edit=edit)
-    log(f"attention unseen NaN {kind} q={q}")
+    if tiles:
+        tiles_bounds(st, by_keys=q > 50)
+    log(f"attention unseen NaN {kind} q={q} tiles={tiles}")
     out, lse = fq.fq_paged_attention(st.q, st.cache, st.batch, return_lse=True)
     torch.cuda.synchronize()
     o, e = f64(out), f64(lse)
@@ -334,6 +422,8 @@ def test_attention_unseen_infinities_and_nan(gpu_lib, kind, q):
             assert np.isnan(o[t, 2:]).all()       # a row that no code can hold reads as NaN
     # the other rows are those of a cache without them
     clean = Step(fq, kind, D, 4, 2, 16, [q], [S], seed=3)
+    if tiles:
+        tiles_bounds(clean, by_keys=q > 50)
     want = fq.fq_paged_attention(clean.q, clean.cache, clean.batch)
     assert torch.equal(out[:q - 2], want[:q - 2])
 
