@@ -16,10 +16,13 @@
 // operand needs 8 keys of one channel, is read as 8 keys x 8 channels a lane and put
 // together by byte permutes, two keys to a register.  Nothing goes through LDS.
 //
-// Quantised caches.  A code c becomes a bf16 exactly (4 bits: 128 + c by one and-or,
-// 8 bits: through fp32), and the affine map is applied to the sums:
+// Quantised caches.  A code c becomes a bf16 exactly (4 bits: 16 + c by one and-or, the
+// smallest offset that takes no more; 8 bits: through fp32), and the affine map is applied
+// to the sums:
 //     q . k = s_k (sum q c - z_k sum q),   sum p v = sum p' c - sum p' z_v,
 //     p' = bf16(p s_v).
+// The offset's own sums cancel in fp32: with 128 + c, a bf16's last bits, the log-sum over
+// three keys was off by 5e-7 of itself, with 16 + c by what it is off in bf16.
 #include <algorithm>
 
 #include "attention.hpp"
@@ -39,6 +42,12 @@ __device__ __forceinline__ int q_channel(int st, int q) {
   if constexpr (KIND == FQ_KV_BF16) return st * 32 + q * 8;
   else if constexpr (KIND == FQ_KV_INT8) return (st >> 1) * 64 + q * 16 + (st & 1) * 8;
   else return q * (D / 4) + st * 8;
+}
+
+// Codes i and 4 + i of a word of eight as the bf16 pair 16 + c.
+constexpr uint32_t kSixteens = 0x41804180u;
+__device__ __forceinline__ uint32_t codes_plus_16(uint32_t w, int i) {
+  return and_or(i == 0 ? w << 3 : w >> (4 * i - 3), 0x00780078u, kSixteens);
 }
 
 // One K row's share of a lane: the codes or bf16 of all its k-slots.
@@ -75,7 +84,7 @@ struct KRow {
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = and_or(w[st] >> (4 * i), 0x000F000Fu, 0x43004300u);
+      for (int i = 0; i < 4; ++i) r[i] = codes_plus_16(w[st], i);
     }
     return __builtin_bit_cast(bf16x8_t, r);
   }
@@ -121,7 +130,7 @@ struct VRows {
                                      0x07060302u);
       } else {
         const uint32_t t = __builtin_amdgcn_perm(b[0], a[0], c < 4 ? 0x05040100u : 0x07060302u);
-        r[i] = and_or(t >> (4 * (c & 3)), 0x000F000Fu, 0x43004300u);
+        r[i] = codes_plus_16(t, c & 3);
       }
     }
     return __builtin_bit_cast(bf16x8_t, r);
@@ -178,7 +187,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) attn_rows_kernel(AttnArgs a) {
   }
   if constexpr (KIND != FQ_KV_BF16) q_sum = row_add(q_sum);
   // the offset of the codes is taken off where the products of K start from
-  const float from = KIND == FQ_KV_INT4 ? -kCodeOffset * q_sum : 0.f;
+  const float from = KIND == FQ_KV_INT4 ? -16.f * q_sum : 0.f;
   const f32x4_t d0{from, from, from, from};
 
   f32x4_t acc[CB];
@@ -269,7 +278,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) attn_rows_kernel(AttnArgs a) {
       if constexpr (KIND != FQ_KV_BF16) {
         const uint32_t w = pw[e];
         corr = dot2_bf16(w, __builtin_amdgcn_perm(vmw[2 * e + 1], vmw[2 * e], 0x07060302u), corr);
-        if constexpr (KIND == FQ_KV_INT4) corr = dot2_bf16(w, 0x43004300u, corr);   // the offset 128
+        if constexpr (KIND == FQ_KV_INT4) corr = dot2_bf16(w, kSixteens, corr);   // the offset
       }
     }
     if constexpr (KIND == FQ_KV_BF16) {
