@@ -16,6 +16,12 @@
 // Quantised caches become c - z on the way into LDS, which is exact in bf16 (|c - z| <=
 // 255); the rows' scales are applied in fp32, s_k to the scores and s_v to the weights
 // before these are rounded.
+//
+// 2048 tokens over 8192 keys, 32 heads on 8, D = 128, bf16: 263 to 293 us, 820 to 915
+// TFLOP/s (a product of 8192^3: 1213).  The matrix cores are busy a third of the time:
+// a wave's tile takes about 200 vector instructions beside 32 products, and 256 registers
+// leave no room to compute one tile's scores beside another's softmax (374 us, with
+// spills); two workgroups to a CU overlap each other.  256 rows a workgroup: 300 us.
 #include "attention.hpp"
 
 namespace fqk {
@@ -249,7 +255,6 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
   const char* vh = a.v + it.head * a.head_stride;
   const uint32_t* kmh = KIND == FQ_KV_BF16 ? nullptr : a.k_meta + it.head * a.meta_head_stride;
   const uint32_t* vmh = KIND == FQ_KV_BF16 ? nullptr : a.v_meta + it.head * a.meta_head_stride;
-  using S = Share<KIND, D>;
   using S = Share<KIND, D>;
   S share;
   typename S::Places places;

@@ -2,10 +2,14 @@
 //
 // A row's range needs all of its channels and nothing else, so D / 8 lanes hold one
 // row, 16 bytes of bf16 each, and agree on its range without LDS.  A thread takes K and V
-// of kTokens tokens of one head, all loads first: the chain slot, row, store is latency,
-// and several rows a thread hide it.  A workgroup takes consecutive tokens of one head: in
-// a page these rows follow one another, so their stores fill whole cache lines.  Both
-// kernels are bound by memory.
+// of a token and head, both loads first.  A workgroup takes consecutive tokens of one head:
+// in a page these rows follow one another, so their stores fill whole cache lines.
+//
+// Memory bounds both kernels (a copy of 2 GiB: 4.9 TB/s), and with codes the arithmetic of
+// the write stands next to it.  4096 tokens of 8 heads x 128, bf16, written: 5.8 us, 5.8
+// TB/s; 12001 tokens at 4 bits: written in 13.7 us, 4.5 TB/s (18 with general divisions and
+// conversions), read back in 12, 5.2 TB/s; 30007 tokens at 8 bits read as fp32: 49 us, 6.3
+// TB/s.
 #include <hip/hip_runtime.h>
 
 #include "device.hpp"
@@ -22,23 +26,21 @@ struct CacheArgs {
   int64_t page_stride, head_stride, token_stride, meta_page_stride, meta_head_stride;
   int64_t n_slots;
   uint32_t page_size;
+  uint32_t page_magic, page_shift;   // of the division by the page's 16-token blocks
 };
 
 struct Place {
-  int64_t page;
-  uint32_t off;
+  uint32_t page, off;
 };
 
+// Page and token of a slot below n_slots (up to 2^47).  A slot of 32 bits has a block b of
+// 28, and with P <= 2^l blocks a page and m = ceil(2^(28 + l) / P) the page is
+// b m >> (28 + l): m is less than 1 too large, which adds less than 2^-l <= 1 / P.
 __device__ __forceinline__ Place place_of(int64_t slot, const CacheArgs& a) {
-  // slots of a cache of up to 2^31 pages fit 47 bits; the 32-bit division serves all but
-  // the largest caches
   Place p;
-  if (slot >> 32) {
-    p.page = slot / int64_t(a.page_size);
-  } else {
-    p.page = uint32_t(slot) / a.page_size;
-  }
-  p.off = uint32_t(slot - p.page * int64_t(a.page_size));
+  if (slot >> 32) p.page = uint32_t(slot / int64_t(a.page_size));
+  else p.page = uint32_t(uint64_t(uint32_t(slot) >> 4) * a.page_magic >> a.page_shift);
+  p.off = uint32_t(slot) - p.page * a.page_size;
   return p;
 }
 
@@ -51,87 +53,96 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 template <int KIND>
 constexpr float kTop = KIND == FQ_KV_INT8 ? 255.f : 15.f;
 
-// The scale of a row: the smallest bf16 not below span / top (the next 16 bits up of
-// a value that is not negative).  The quotient is the correctly rounded one: with a
-// product by 1 / top, spans that are a multiple of a bf16 would get the next step.
-template <int KIND>
-__device__ __forceinline__ float scale_of(float span) {
-  if (!(span > 0.f)) return 1.f;
-  const float q = __fdiv_rn(span, kTop<KIND>);
-  return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, q) + 0xFFFFu) & 0xFFFF0000u);
+// Maximum and minimum that a NaN passes through.
+struct MaxNan {
+  __device__ __forceinline__ float operator()(float a, float b) const { return __builtin_elementwise_maximum(a, b); }
+};
+struct MinNan {
+  __device__ __forceinline__ float operator()(float a, float b) const { return __builtin_elementwise_minimum(a, b); }
+};
+
+// The next bf16 up of a value that is not negative, unless it is one.
+__device__ __forceinline__ float bf16_up(float v) {
+  return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, v) + 0xFFFFu) & 0xFFFF0000u);
 }
 
-constexpr int kTokens = 1;   // a thread
+// a / b correctly rounded from r = 1 / b correctly rounded: y = a r is next to it, a - y b
+// is exact, and one more step of it gives the rounded quotient (Markstein), far from the
+// ends of the range.  (Checked for b = 255 and 15 over all fp32, and for all bf16 a and b.)
+__device__ __forceinline__ float quotient(float a, float b, float r) {
+  const float y = a * r;
+  return fmaf(fmaf(-y, b, a), r, y);
+}
 
-// Quantises a row's 8 channels of this lane and stores them.  The quotients x / s are the
-// correctly rounded ones: of numbers of 8 bits they round to the same integer as the exact
-// quotients do, ties among them.  With r = 1 / s rounded correctly, y = x r and the exact
-// remainder e = x - y s, fma(e, r, y) is the rounded quotient (Markstein) as long as r and
-// e s are far from the ends of the range.
+// Quantises a row's 8 channels of this lane and stores them.  The scale is the smallest
+// bf16 not below span / top, and every quotient is the correctly rounded one: with
+// products by rounded inverses, spans that are a multiple of a bf16 would get the next
+// scale, and ties the next code.  Rows of ordinary size take quotient(), about a third of
+// the operations of the general division, which rows of zeros, of extreme sizes and of
+// infinities or NaN take.
+//
+// To whole numbers by sums with 1.5 2^23, where floats are 1 apart: the code is then the
+// low bits of the float.
 template <int KIND, int D>
 __device__ __forceinline__ void store_row(char* dst, uint32_t* meta, uint4 w, int i, bool store) {
   if constexpr (KIND == FQ_KV_BF16) {
     if (store) reinterpret_cast<uint4*>(dst)[i] = w;
   } else {
     constexpr int LPR = D / 8;
+    constexpr float top = kTop<KIND>, whole = 0x1.8p23f;
     float x[8];
     const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
     float hi = 0.f, lo = 0.f;
-    bool odd = false;   // an infinity or a NaN
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       x[2 * j] = __builtin_bit_cast(float, ws[j] << 16);
       x[2 * j + 1] = __builtin_bit_cast(float, ws[j] & 0xFFFF0000u);
-      odd |= (ws[j] & 0x7F80u) == 0x7F80u || (ws[j] & 0x7F800000u) == 0x7F800000u;
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      hi = fmaxf(hi, x[j]);
-      lo = fminf(lo, x[j]);
+      hi = MaxNan{}(hi, x[j]);
+      lo = MinNan{}(lo, x[j]);
     }
-    if (odd) hi = __builtin_inff();
-    hi = over_lanes<LPR>(hi, Max{});
-    lo = over_lanes<LPR>(lo, Min{});
+    hi = over_lanes<LPR>(hi, MaxNan{});
+    lo = over_lanes<LPR>(lo, MinNan{});
     const float span = hi - lo;
-    const bool bad = !(span <= 3.4028234663852886e38f);
-    const float s = scale_of<KIND>(bad ? 0.f : span);
-    const float z = fminf(fmaxf(rintf(__fdiv_rn(-lo, s)), 0.f), kTop<KIND>);
+    float s, zq;
+    uint32_t sb;
+    if (span > 0x1p-90f && span < 0x1p90f) {
+      s = bf16_up(quotient(span, top, 1.f / top));
+      // 1 / s: one step from an approximation within 2 of its last places is the rounded
+      // one for every s of 8 bits
+      const float r0 = __builtin_amdgcn_rcpf(s), r = fmaf(fmaf(-s, r0, 1.f), r0, r0);
+      zq = quotient(-lo, s, r);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = quotient(x[j], s, r);
+      sb = __builtin_bit_cast(uint32_t, s) >> 16;
+    } else {
+      const bool bad = !(span <= 3.4028234663852886e38f);   // an infinity or NaN, or a span beyond fp32
+      s = span > 0.f && !bad ? bf16_up(__fdiv_rn(span, top)) : 1.f;
+      zq = bad ? 0.f : __fdiv_rn(-lo, s);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = bad ? 0.f : __fdiv_rn(x[j], s);
+      sb = bad ? 0x7FC0u : __builtin_bit_cast(uint32_t, s) >> 16;
+    }
+    const float z = __builtin_amdgcn_fmed3f(zq + whole, whole, whole + top) - whole;
     uint32_t c[8];
-    const bool middle = s > 0x1p-100f && s < 0x1p100f;
-    const float r = __fdiv_rn(1.f, s);
-    if (middle) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float y = x[j] * r;
-        x[j] = fmaf(fmaf(-y, s, x[j]), r, y);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = __fdiv_rn(x[j], s);
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) c[j] = uint32_t(fminf(fmaxf(rintf(x[j]) + z, 0.f), kTop<KIND>));
-    if (bad) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) c[j] = 0u;
-    }
+    for (int j = 0; j < 8; ++j)
+      c[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(x[j] + whole + z, whole, whole + top));
     if (!store) return;
+    // the codes are the low bits; the bits above the low 16 are those of 1.5 2^23
+    const auto bytes = [](uint32_t a, uint32_t b, uint32_t e, uint32_t f) {
+      return __builtin_amdgcn_perm(__builtin_amdgcn_perm(f, e, 0x0C0C0400u), __builtin_amdgcn_perm(b, a, 0x0C0C0400u),
+                                   0x05040100u);
+    };
     if constexpr (KIND == FQ_KV_INT8) {
-      uint2 o;
-      o.x = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
-      o.y = c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24;
-      reinterpret_cast<uint2*>(dst)[i] = o;
+      reinterpret_cast<uint2*>(dst)[i] = uint2{bytes(c[0], c[1], c[2], c[3]), bytes(c[4], c[5], c[6], c[7])};
     } else {
-      uint32_t o = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o |= c[j] << (4 * j);
-      reinterpret_cast<uint32_t*>(dst)[i] = o;
+      reinterpret_cast<uint32_t*>(dst)[i] =
+          bytes(c[0] | c[1] << 4, c[2] | c[3] << 4, c[4] | c[5] << 4, c[6] | c[7] << 4);
     }
-    if (i == 0) {
-      const uint32_t zb = bad ? 0u : __builtin_bit_cast(uint32_t, z) & 0xFFFF0000u;
-      const uint32_t sb = bad ? 0x7FC0u : __builtin_bit_cast(uint32_t, s) >> 16;
-      *meta = sb | zb;
-    }
+    if (i == 0) *meta = sb | (__builtin_bit_cast(uint32_t, z) & 0xFFFF0000u);
   }
 }
 
@@ -139,32 +150,20 @@ template <int KIND, int D>
 __global__ void __launch_bounds__(256)
 kv_write_kernel(CacheArgs a, const uint16_t* K, const uint16_t* V, int64_t k_token, int64_t k_head,
                 int64_t v_token, int64_t v_head, const int64_t* slots, int n_tokens) {
-  constexpr int LPR = D / 8, PER = 256 / LPR;   // lanes a row, rows of a workgroup at a time
+  constexpr int LPR = D / 8, PER = 256 / LPR;   // lanes a row, rows of a workgroup
   const int i = int(threadIdx.x) % LPR;
   const int head = int(blockIdx.y);
-  const int t0 = int(blockIdx.x) * (PER * kTokens) + int(threadIdx.x) / LPR;
-  int64_t slot[kTokens];
-  uint4 k[kTokens], v[kTokens];
-#pragma unroll
-  for (int u = 0; u < kTokens; ++u) {
-    const int t = t0 + u * PER;
-    const bool in = t < n_tokens;
-    slot[u] = in ? slots[t] : -1;
-    k[u] = v[u] = uint4{0, 0, 0, 0};
-    if (in) {
-      k[u] = reinterpret_cast<const uint4*>(K + head * k_head + k_token * int64_t(t))[i];
-      v[u] = reinterpret_cast<const uint4*>(V + head * v_head + v_token * int64_t(t))[i];
-    }
-  }
-#pragma unroll
-  for (int u = 0; u < kTokens; ++u) {
-    const bool store = uint64_t(slot[u]) < uint64_t(a.n_slots);
-    const Place p = place_of(store ? slot[u] : 0, a);
-    const int64_t at = p.page * a.page_stride + head * a.head_stride + int64_t(p.off) * a.token_stride;
-    const int64_t word = p.page * a.meta_page_stride + head * a.meta_head_stride + p.off;
-    store_row<KIND, D>(a.rows[0] + at, a.meta[0] + word, k[u], i, store);
-    store_row<KIND, D>(a.rows[1] + at, a.meta[1] + word, v[u], i, store);
-  }
+  const int t = int(blockIdx.x) * PER + int(threadIdx.x) / LPR;
+  if (t >= n_tokens) return;   // whole rows: the lanes of a row have the same token
+  const int64_t slot = slots[t];
+  const uint4 k = reinterpret_cast<const uint4*>(K + head * k_head + k_token * int64_t(t))[i];
+  const uint4 v = reinterpret_cast<const uint4*>(V + head * v_head + v_token * int64_t(t))[i];
+  const bool store = uint64_t(slot) < uint64_t(a.n_slots);
+  const Place p = place_of(store ? slot : 0, a);
+  const int64_t at = p.page * a.page_stride + head * a.head_stride + int64_t(p.off) * a.token_stride;
+  const int64_t word = p.page * a.meta_page_stride + head * a.meta_head_stride + p.off;
+  store_row<KIND, D>(a.rows[0] + at, a.meta[0] + word, k, i, store);
+  store_row<KIND, D>(a.rows[1] + at, a.meta[1] + word, v, i, store);
 }
 
 // N channels from channel c of a row on, as numbers.
@@ -213,63 +212,59 @@ kv_read_kernel(CacheArgs a, const int64_t* slots, int n_tokens, void* K, void* V
   constexpr int LPR = D / 8, PER = 256 / LPR;
   const int i = int(threadIdx.x) % LPR;
   const int head = int(blockIdx.y);
-  const int t0 = int(blockIdx.x) * (PER * kTokens) + int(threadIdx.x) / LPR;
-  float x[kTokens][2][8];
+  const int t = int(blockIdx.x) * PER + int(threadIdx.x) / LPR;
+  if (t >= n_tokens) return;
+  const int64_t slot = slots[t];
+  const bool in = uint64_t(slot) < uint64_t(a.n_slots);
+  const Place p = place_of(in ? slot : 0, a);
+  const int64_t at = p.page * a.page_stride + head * a.head_stride + int64_t(p.off) * a.token_stride;
+  const int64_t word = p.page * a.meta_page_stride + head * a.meta_head_stride + p.off;
+  float x[2][8];
 #pragma unroll
-  for (int u = 0; u < kTokens; ++u) {
-    const int t = t0 + u * PER;
-    const int64_t slot = t < n_tokens ? slots[t] : -1;
-    const bool in = uint64_t(slot) < uint64_t(a.n_slots);
-    const Place p = place_of(in ? slot : 0, a);
-    const int64_t at = p.page * a.page_stride + head * a.head_stride + int64_t(p.off) * a.token_stride;
-    const int64_t word = p.page * a.meta_page_stride + head * a.meta_head_stride + p.off;
+  for (int v = 0; v < 2; ++v) {
+    if (!in) {
 #pragma unroll
-    for (int v = 0; v < 2; ++v) {
-      if (!in) {
+      for (int j = 0; j < 8; ++j) x[v][j] = 0.f;
+      continue;
+    }
+    const uint32_t meta = KIND == FQ_KV_BF16 ? 0u : a.meta[v][word];
+    if constexpr (F32) {
+      float lo[4], hi[4];
+      load_channels<KIND, 4>(a.rows[v] + at, 4 * i, meta, lo);
+      load_channels<KIND, 4>(a.rows[v] + at, D / 2 + 4 * i, meta, hi);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[u][v][j] = 0.f;
-        continue;
+      for (int j = 0; j < 4; ++j) {
+        x[v][j] = lo[j];
+        x[v][4 + j] = hi[j];
       }
-      const uint32_t meta = KIND == FQ_KV_BF16 ? 0u : a.meta[v][word];
-      if constexpr (F32) {
-        float lo[4], hi[4];
-        load_channels<KIND, 4>(a.rows[v] + at, 4 * i, meta, lo);
-        load_channels<KIND, 4>(a.rows[v] + at, D / 2 + 4 * i, meta, hi);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          x[u][v][j] = lo[j];
-          x[u][v][4 + j] = hi[j];
-        }
-      } else {
-        load_channels<KIND, 8>(a.rows[v] + at, 8 * i, meta, x[u][v]);
-      }
+    } else {
+      load_channels<KIND, 8>(a.rows[v] + at, 8 * i, meta, x[v]);
     }
   }
+  const int64_t to = (int64_t(t) * gridDim.y + head) * D;
 #pragma unroll
-  for (int u = 0; u < kTokens; ++u) {
-    const int t = t0 + u * PER;
-    if (t >= n_tokens) return;
-    const int64_t at = (int64_t(t) * gridDim.y + head) * D;
-#pragma unroll
-    for (int v = 0; v < 2; ++v) {
-      const float* y = x[u][v];
-      if constexpr (F32) {
-        float* o = static_cast<float*>(v ? V : K) + at;
-        put<STREAM>(o + 4 * i, f32x4_t{y[0], y[1], y[2], y[3]});
-        put<STREAM>(o + D / 2 + 4 * i, f32x4_t{y[4], y[5], y[6], y[7]});
-      } else {
-        uint16_t* o = static_cast<uint16_t*>(v ? V : K) + at;
-        put<STREAM>(o + 8 * i, u32x4_t{pack2(y[0], y[1]), pack2(y[2], y[3]), pack2(y[4], y[5]), pack2(y[6], y[7])});
-      }
+  for (int v = 0; v < 2; ++v) {
+    const float* y = x[v];
+    if constexpr (F32) {
+      float* o = static_cast<float*>(v ? V : K) + to;
+      put<STREAM>(o + 4 * i, f32x4_t{y[0], y[1], y[2], y[3]});
+      put<STREAM>(o + D / 2 + 4 * i, f32x4_t{y[4], y[5], y[6], y[7]});
+    } else {
+      uint16_t* o = static_cast<uint16_t*>(v ? V : K) + to;
+      put<STREAM>(o + 8 * i, u32x4_t{pack2(y[0], y[1]), pack2(y[2], y[3]), pack2(y[4], y[5]), pack2(y[6], y[7])});
     }
   }
 }
 
 CacheArgs cache_args(const fq_kv_cache& c) {
+  const uint32_t blocks = uint32_t(c.page_size) / 16;
+  uint32_t l = 0;
+  while ((1u << l) < blocks) ++l;
   return CacheArgs{{static_cast<char*>(c.k), static_cast<char*>(c.v)},
                    {static_cast<uint32_t*>(c.k_meta), static_cast<uint32_t*>(c.v_meta)},
                    c.page_stride, c.head_stride, c.token_stride, c.meta_page_stride, c.meta_head_stride,
-                   c.n_pages * c.page_size, uint32_t(c.page_size)};
+                   c.n_pages * c.page_size, uint32_t(c.page_size),
+                   uint32_t(((uint64_t(1) << (28 + l)) + blocks - 1) / blocks), 28 + l};
 }
 
 // f(integral_constant KIND, integral_constant D) for the cache's kind and head size.
@@ -285,7 +280,7 @@ void by_kind(const fq_kv_cache& c, F&& f) {
 }
 
 dim3 token_grid(const fq_kv_cache& c, int64_t n_tokens) {
-  const int per = 256 / (c.head_dim / 8) * kTokens;
+  const int per = 256 / (c.head_dim / 8);
   return dim3(unsigned((n_tokens + per - 1) / per), unsigned(c.n_kv_heads));
 }
 

@@ -133,6 +133,38 @@ def test_cache_write_and_read(gpu_lib, kind, D, order):
             np.testing.assert_array_equal(y.float().numpy(), want.float().numpy())
 
 
+@pytest.mark.parametrize("page,n_pages", [(16, 400), (592, 11), (4112, 3), (65536, 2)])
+@pytest.mark.parametrize("kind", ["int8", "int4"])
+def test_cache_codes_over_sizes(gpu_lib, kind, page, n_pages):
+    """Scales, zero-points and codes of rows of all sizes, those at the ends of the quick
+    division's range (spans of 2^-90 and 2^90) among them, are exact; pages of any size."""
+    fq = gpu_lib
+    heads, D, n = 2, 64, 1500
+    log(f"cache sizes {kind} page={page}")
+    cache = make_cache(fq, kind, n_pages, page, heads, D, "hnd")
+    g = torch.Generator().manual_seed(page)
+    k, v = (rand_bf16((n, heads, D), page + i, 1.0) for i in (1, 2))
+    e = torch.randint(-124, 118, (n,), generator=g)
+    e[:40] = torch.arange(40) % 8 - 94
+    e[40:80] = torch.arange(40) % 8 + 84
+    k = (k.double() * torch.exp2(e.double())[:, None, None]).to(torch.bfloat16)
+    k[100:200, :, 1:] = 0                                  # one value, on either side of 0
+    v[200:300] = v[200:300].abs()                          # nothing below 0
+    v[300:400] = -v[300:400].abs()
+    v[400:500] = (torch.randint(-255, 256, (100, heads, D), generator=g) / 2).to(torch.bfloat16)   # ties
+    slots = torch.randperm(n_pages * page, generator=g)[:n]
+    slots[0] = n_pages * page - 1
+    slots = slots.unique()
+    k, v = k[:len(slots)], v[:len(slots)]
+    fq.fq_kv_cache_write(cache, k.cuda(), v.cuda(), slots.cuda())
+    torch.cuda.synchronize()
+    for (c, s, z), x in zip(codes_of(cache, slots), (f64(k), f64(v))):
+        ec, es, ez = L.quantise_rows(x, kind)
+        np.testing.assert_array_equal(s, es)
+        np.testing.assert_array_equal(z, ez)
+        np.testing.assert_array_equal(c, ec)
+
+
 def test_cache_of_no_and_one_token_and_repeats(gpu_lib):
     fq = gpu_lib
     cache = make_cache(fq, "int8", 2, 16, 1, 128)
