@@ -627,8 +627,7 @@ fq_status fq_paged_attention(const fq_attention* a, const uint16_t* Q, const fq_
  *   residual_out    device, residual_dtype: r; may be residual itself; NULL: not written.
  *   h               device bf16; NULL: not computed.
  * One of residual_out and h at least.  Strides are of rows, in elements; columns are
- * contiguous.  Any alignment of the element's own size is accepted; rows that are all
- * 16-byte aligned (with cols a multiple of 8) are read in wide loads.
+ * contiguous.  Any alignment of the element's own size is accepted.
  * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE, FQ_ERR_UNSUPPORTED, FQ_ERR_ALIGN, FQ_ERR_HIP.
  */
 typedef struct {

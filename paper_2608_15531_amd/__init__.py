@@ -943,6 +943,8 @@ def fq_gated_residual_norm(x, residual=None, pre_weight=None, post_weight=None, 
     lib = load()
     if not isinstance(x, torch.Tensor) or x.dim() != 2:
         raise ValueError("x: expected [rows][cols]")
+    if not x.is_cuda:   # below, the others are only compared with its device
+        raise TypeError("x must be a CUDA (HIP) tensor")
     index, bf16, shape, xt = x.get_device(), torch.bfloat16, x.shape, x.dtype
     M, H = shape
     xs = _rows(x, xt, shape, "x", index)

@@ -210,6 +210,13 @@ def test_binding_refuses():
         fq.fq_gated_residual_norm(t)
 
 
+def test_norm_refuses_host_tensors(lib):
+    torch = pytest.importorskip("torch")
+    x, w = torch.zeros((2, 64), dtype=torch.bfloat16), torch.ones(64, dtype=torch.bfloat16)
+    with pytest.raises(TypeError, match="CUDA"):
+        fq.fq_gated_residual_norm(x, x, w)
+
+
 # ----------------------------------------------------------- oracle pins --
 
 def test_oracle_bf16_ceil():
