@@ -491,6 +491,10 @@ constexpr int kRangeCost = 4;
 // Partial results are kept small: 2048 ranges of 128 rows are 138 MB, 8192 of 16 rows 69.
 constexpr int kMostTileRanges = 2048, kMostRanges = 8192;
 
+// Keys are numbered below 2^28, so a wider window sees the same ones; positions before the
+// first key less the window stay in 32 bits.
+constexpr int kWidestWindow = 1 << 30;
+
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace
@@ -579,7 +583,7 @@ int launch_attention(const AttnPlan& pl, const fq_attention& a, const fq_kv_cach
   g.n_kv_heads = c.n_kv_heads;
   g.max_q = a.max_q;
   g.max_kv = a.max_kv;
-  g.window = a.window;
+  g.window = std::min(a.window, kWidestWindow);
   g.sinks = a.sinks;
   g.row_blocks = pl.row_blocks;
   g.split = pl.split;

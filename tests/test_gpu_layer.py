@@ -515,6 +515,20 @@ def test_attention_bounds_above_the_lengths(gpu_lib):
     st.check(torch.cat([keep[:3], out[3:]]), None, 0, 0)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+@pytest.mark.parametrize("window", [1 << 30, 2**31 - 1])
+def test_attention_widest_windows(gpu_lib, window, kind):
+    """Windows at the end of their type see what no window sees, with tokens before the first
+    key in the same wave as others."""
+    fq = gpu_lib
+    st = Step(fq, kind, 128, 2, 2, 16, [140, 20], [130, 5], seed=21)
+    c = tiles_bounds(st, window)
+    log(f"attention window {window} {kind} {c}")
+    out, lse = fq.fq_paged_attention(st.q, st.cache, st.batch, window=window, return_lse=True)
+    torch.cuda.synchronize()
+    st.check(out, lse, 0, 0)
+
+
 def test_attention_offsets_beyond_32_bits(gpu_lib):
     """Pages that start beyond 4 GiB of the pool, and slots there."""
     fq = gpu_lib
