@@ -127,7 +127,7 @@ struct Share {
   // would wait for it before any LDS read, of the other tile too.)
   __device__ static __forceinline__ void to_lds(const char* p, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
-                 :: "v"(p), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory");
+                 :: "v"(p), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
   }
 
   template <int W>

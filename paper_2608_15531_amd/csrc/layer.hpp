@@ -34,7 +34,7 @@ struct AttnPlan {
 // The arguments have been checked; false: sizes beyond what the kernels index.
 bool plan_attention(const fq_attention& a, const fq_kv_cache& c, AttnPlan* plan);
 
-// Each enqueues one kernel and returns a hipError_t value (0 on success).
+// Each enqueues its kernel (attention over many rows also that of the join) and returns a hipError_t value (0 on success).
 int launch_attention(const AttnPlan& plan, const fq_attention& a, const fq_kv_cache& c,
                      const uint16_t* Q, const int32_t* cu_q, const int32_t* kv_lens,
                      const int32_t* table, uint16_t* O, float* lse, void* workspace,
