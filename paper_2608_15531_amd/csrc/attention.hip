@@ -354,7 +354,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) attn_rows_kernel(AttnArgs a) {
 
   if (it.n_parts > 1) {
     // partial sums: [item][range][row][D] floats, then [item][range][row][2]
-    const int64_t item = (int64_t(it.seq) * a.n_kv_heads + it.head) * a.row_blocks + it.rb;
+    const int64_t item = it.number;
     const uint32_t part_words = uint32_t(a.part_rows) * (D + 4);
     float* base_p = a.partials + item * a.split * part_words;
     const __amdgpu_buffer_rsrc_t prs = make_rsrc(base_p, uint32_t(a.split) * part_words * 4u);
@@ -484,10 +484,12 @@ constexpr int kEvenRanges = 8, kEvenMinTiles = 24, kEvenMaxTiles = 128;
 // 34 / 28.
 constexpr int64_t kFewRowsBytes = int64_t(224) << 20;
 // The kernel for many rows has two workgroups to a CU; it splits the keys where that makes
-// rounds * (tiles of a range + kRangeCost) smaller, a range's start and its part in the join
-// being worth so many tiles.
+// rounds * (tiles of a range + kRangeCost) + bytes of the partial sums / kTileBytes smaller:
+// a range's start and its part in the join are worth so many tiles, and in a tile's time, 2.3
+// us, that many bytes are written and read again.
 constexpr int kTileSlots = 512;
 constexpr int kRangeCost = 4;
+constexpr int64_t kTileBytes = int64_t(5) << 20;
 // Partial results are kept small: 2048 ranges of 128 rows are 138 MB, 8192 of 16 rows 69.
 constexpr int kMostTileRanges = 2048, kMostRanges = 8192;
 
@@ -512,7 +514,20 @@ bool plan_attention(const fq_attention& a, const fq_kv_cache& c, AttnPlan* pl) {
   const int64_t row_blocks = ceil_div(rows, pl->rows);
   if (row_blocks > (1 << 24) || a.n_seqs > 65535) return false;
   pl->row_blocks = int(row_blocks);
-  const int64_t items = row_blocks * c.n_kv_heads * a.n_seqs;
+  const int64_t grid = row_blocks * c.n_kv_heads * a.n_seqs;
+  // Of those, the ones that can hold rows: in the kernel for many rows sequences of very
+  // different lengths are common.  (The one for few keeps a counter for each by its place in
+  // the grid, which no content of cu_q can make two blocks share.)
+  int64_t blocks = row_blocks * a.n_seqs;
+  pl->dense_blocks = 0;
+  if (pl->kernel == FQ_ATTN_TILES && a.total_q / pl->rows < blocks) {
+    const int64_t dense = a.total_q * group / pl->rows + a.n_seqs;
+    if (dense < blocks) {
+      blocks = dense;
+      pl->dense_blocks = 1;
+    }
+  }
+  const int64_t items = blocks * c.n_kv_heads;
   // tiles that a block of rows can see at most: those of the first keys, and a window of
   // every token of the block, at any place
   int64_t tiles = ceil_div(a.max_kv, pl->tile);
@@ -522,7 +537,11 @@ bool plan_attention(const fq_attention& a, const fq_kv_cache& c, AttnPlan* pl) {
   int64_t split = 1;
   if (items <= kMaxStrips) {   // every item has a counter
     if (pl->kernel == FQ_ATTN_TILES) {
-      const auto cost = [&](int64_t n) { return ceil_div(items * n, kTileSlots) * (ceil_div(tiles, n) + kRangeCost); };
+      const int64_t range_bytes = std::min<int64_t>(pl->rows, rows) * (c.head_dim + 4) * 4;
+      const auto cost = [&](int64_t n) {
+        return ceil_div(items * n, kTileSlots) * (ceil_div(tiles, n) + kRangeCost) +
+               (n > 1 ? items * n * range_bytes / kTileBytes : 0);
+      };
       for (int64_t n = 2; n <= std::min<int64_t>(tiles / 2, 64) && items * n <= kMostTileRanges; ++n)
         if (cost(n) < cost(split)) split = n;
     } else {
@@ -536,7 +555,7 @@ bool plan_attention(const fq_attention& a, const fq_kv_cache& c, AttnPlan* pl) {
   pl->split_tiles = int(ceil_div(tiles, split));
   pl->split = int(ceil_div(tiles, pl->split_tiles));
   if (pl->split * row_blocks * c.n_kv_heads > INT32_MAX) return false;
-  pl->workgroups = items * pl->split;
+  pl->workgroups = grid * pl->split;
   if (pl->workgroups > INT32_MAX) return false;
   if (pl->kernel == FQ_ATTN_TILES) pl->lds_bytes = fqk::attn_tiles_lds(c.head_dim);
   else pl->lds_bytes = c.head_dim == 64 ? fqk::kAttnLds<64> : fqk::kAttnLds<128>;
@@ -589,6 +608,7 @@ int launch_attention(const AttnPlan& pl, const fq_attention& a, const fq_kv_cach
   g.split = pl.split;
   g.split_tiles = pl.split_tiles;
   g.part_rows = pl.part_rows;
+  g.dense_blocks = pl.dense_blocks;
   g.scale_log2 = a.scale * 1.44269504088896340736f;
   const dim3 grid(unsigned(int64_t(pl.row_blocks) * pl.split * c.n_kv_heads), unsigned(a.n_seqs));
   const hipStream_t s = static_cast<hipStream_t>(stream);

@@ -39,6 +39,7 @@ struct AttnArgs {
   int n_heads, n_kv_heads;
   int max_q, max_kv, window, sinks;
   int row_blocks, split, split_tiles, part_rows;
+  int dense_blocks;        // how blocks are numbered: by the rows before, or row_blocks a sequence
   float scale_log2;        // scale * log2(e): the softmax runs in powers of two
 };
 
@@ -105,6 +106,7 @@ struct Item {
   int64_t t0;          // first new token of the sequence
   uint32_t row0;       // first row of the block (the plan keeps rows below 2^31)
   int rows;
+  int64_t number;      // among all blocks and heads
   int p0;              // position of the sequence's first new token
   int tok_hi;          // the block's last token
   int kv_seen;
@@ -128,6 +130,9 @@ struct Item {
     rows = int(min(n_rows - row0, uint32_t(ROWS)));
     const int tok_lo = int(row0 / group);
     tok_hi = int((row0 + rows - 1) / group);
+    // by the rows before: a sequence whose rows are r .. s - 1 has at most as many blocks as
+    // s / ROWS - r / ROWS + 1
+    number = ((a.dense_blocks ? t0 * a.group / ROWS + seq : int64_t(seq) * a.row_blocks) + rb) * a.n_kv_heads + head;
     p0 = kv_len - q_all;
     kv_seen = min(kv_len, a.max_kv);
     p_lo = min(p0 + tok_lo, kv_seen - 1);

@@ -428,7 +428,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
   l = pair_add(l);
   if (it.n_parts > 1) {
     // partial sums for join_kernel: [item][range][row][D + 4] floats, the last four: m c2, l
-    const int64_t item = (int64_t(it.seq) * a.n_kv_heads + it.head) * a.row_blocks + it.rb;
+    const int64_t item = it.number;
     if (!mine.in) return;
     float* to = a.partials + ((item * a.split + it.part) * a.part_rows + wave * 32 + r32) * (D + 4);
 #pragma unroll
@@ -471,7 +471,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttnArgs a) {
   const int n = it.parts(a);
   const int r = first + int(threadIdx.x) / T, ch = int(threadIdx.x) % T * 8;
   if (n <= 1 || r >= it.rows) return;
-  const int64_t item = (int64_t(it.seq) * a.n_kv_heads + it.head) * a.row_blocks + it.rb;
+  const int64_t item = it.number;
   const int64_t step = int64_t(a.part_rows) * (D + 4);
   const float* from = a.partials + item * a.split * step + int64_t(r) * (D + 4);
   constexpr int U = 8;   // ranges read at a time

@@ -26,6 +26,7 @@ struct AttnPlan {
   int tile;          // keys of a tile
   int split_tiles;   // tiles in a range
   int part_rows;     // rows of a partial result
+  int dense_blocks;  // blocks of rows are numbered without gaps for shorter sequences
   int64_t workgroups;
   size_t lds_bytes;
   size_t partial_bytes, ws_bytes;   // beyond the counters; with them

@@ -173,6 +173,22 @@ def test_attention_plans_cover_the_keys(lib, heads, head_dim):
                         assert len(set((j[see] // 32).tolist())) <= out[3] * (out[4] // 32), (max_q, max_kv, window)
 
 
+@pytest.mark.parametrize("group", [1, 3, 4, 8, 24])
+def test_attention_blocks_of_many_rows_are_numbered_once(group):
+    """The numbers that the kernel for many rows gives its blocks (the rows before them / 128
+    + the sequence + the block) differ and stay below total rows / 128 + sequences, whatever
+    the lengths."""
+    rng = np.random.default_rng(group)
+    for case in range(300):
+        q = rng.integers(0, [2, 40, 400][case % 3], int(rng.integers(1, 12)))
+        max_q = int(q.max()) if case % 2 else int(rng.integers(1, 400))
+        cu = np.concatenate([[0], np.cumsum(q)])
+        seen = [cu[b] * group // 128 + b + rb for b in range(len(q))
+                for rb in range(-(-min(int(q[b]), max_q) * group // 128))]
+        assert len(set(seen)) == len(seen)
+        assert all(0 <= n < cu[-1] * group // 128 + len(q) for n in seen)
+
+
 def test_norm_refuses(lib):
     def call(x=FAKE, res=FAKE, post=FAKE, gate=FAKE, pre=FAKE, out=FAKE, h=FAKE, **kw):
         d = dict(rows=4, cols=128, x_dtype=0, residual_dtype=0, eps=1e-5, residual_scale=1.0, x_stride=128,
