@@ -487,11 +487,20 @@ constexpr int64_t kFewRowsBytes = int64_t(224) << 20;
 // rounds * (tiles of a range + kRangeCost) + bytes of the partial sums / kTileBytes smaller:
 // a range's start and its part in the join are worth so many tiles, and in a tile's time, 2.3
 // us, that many bytes are written and read again.
+// (Up to 2048 ranges: with more of them, not all of the longest sequence's length, the rounds
+// say little; 20 to 900 tokens of 8 sequences over 500 to 8000 keys went from 546 to 678 us.)
 constexpr int kTileSlots = 512;
 constexpr int kRangeCost = 4;
+constexpr int kRoundsRanges = 2048;
 constexpr int64_t kTileBytes = int64_t(5) << 20;
-// Partial results are kept small: 2048 ranges of 128 rows are 138 MB, 8192 of 16 rows 69.
-constexpr int kMostTileRanges = 2048, kMostRanges = 8192;
+// Of several sequences one may be much longer than the others, and its ranges then are what
+// takes long: they have 10240 keys at most.  (us, without / with: 5 to 300 tokens of 6
+// sequences over 500 to 30000 keys, 8 bits: 1126 / 655; 2000, 10 and 100 over 0, 8000 and
+// 20000, 4 bits, 64 heads: 969 / 710; but 4 times 1024 over 16000, 8 bits: 1549 / 1583.  With
+// 4096 keys 20 to 900 tokens of 8 sequences over 500 to 8000 went from 603 to 633.)
+constexpr int64_t kEvenTiles = 160;
+// Partial results are bounded: 4096 ranges of 128 rows are 277 MB, 8192 of 16 rows 69.
+constexpr int64_t kMostTileRanges = 4096, kMostRanges = 8192;
 
 // Keys are numbered below 2^28, so a wider window sees the same ones; positions before the
 // first key less the window stay in 32 bits.
@@ -542,7 +551,8 @@ bool plan_attention(const fq_attention& a, const fq_kv_cache& c, AttnPlan* pl) {
         return ceil_div(items * n, kTileSlots) * (ceil_div(tiles, n) + kRangeCost) +
                (n > 1 ? items * n * range_bytes / kTileBytes : 0);
       };
-      for (int64_t n = 2; n <= std::min<int64_t>(tiles / 2, 64) && items * n <= kMostTileRanges; ++n)
+      if (a.n_seqs > 1) split = std::max<int64_t>(1, std::min(ceil_div(tiles, kEvenTiles), kMostTileRanges / items));
+      for (int64_t n = split + 1; n <= std::min<int64_t>(tiles / 2, 64) && items * n <= kRoundsRanges; ++n)
         if (cost(n) < cost(split)) split = n;
     } else {
       if (items < kTargetWorkgroups)
