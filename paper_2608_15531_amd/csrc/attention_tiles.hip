@@ -18,7 +18,7 @@
 // before these are rounded.
 //
 // 2048 tokens over 8192 keys, 32 heads on 8, D = 128, bf16: 263 to 293 us, 820 to 915
-// TFLOP/s (a product of 8192^3: 1213).  The matrix cores are busy a third of the time:
+// TFLOP/s (a product of 8192^3: 1213).  The matrix cores are busy 39 % of the time:
 // a wave's tile takes about 200 vector instructions beside 32 products, and 256 registers
 // leave no room to compute one tile's scores beside another's softmax (374 us, with
 // spills); two workgroups to a CU overlap each other.  256 rows a workgroup: 300 us.
