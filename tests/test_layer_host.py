@@ -233,6 +233,21 @@ def test_norm_refuses_host_tensors(lib):
         fq.fq_gated_residual_norm(x, x, w)
 
 
+@pytest.mark.parametrize("name", ["max_q", "max_kv", "window", "sinks"])
+def test_numbers_beyond_32_bits_are_refused(name):
+    from types import SimpleNamespace
+    v = dict(max_q=1, max_kv=500, window=0, sinks=0)
+    cache = SimpleNamespace(head_dim=128)
+
+    def call(v):
+        batch = SimpleNamespace(n_seqs=1, max_q=v["max_q"], max_kv=v["max_kv"], table_stride=10, _table_cols=10)
+        return fq._attention(8, (1024, 128), (1024, 128), 1, cache, batch, None, v["window"], v["sinks"])
+
+    assert getattr(call({**v, name: 2**31 - 1}), name) == 2**31 - 1
+    with pytest.raises(ValueError):
+        call({**v, name: 2**32 + 5})
+
+
 # ----------------------------------------------------------- oracle pins --
 
 def test_oracle_bf16_ceil():
