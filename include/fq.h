@@ -464,7 +464,8 @@ fq_status fq_debug_decode_tile_coo(const fq_tilecoo_dev* tc, int32_t K, int32_t 
  * A row of codes c has a scale s and a zero-point z of its own and stands for
  * s (c - z).  s and z are the two bf16 of one 4-byte word (s in the low half) of
  * k_meta or v_meta.  bf16 for s, since it has the range of the activations;
- * integers up to 255 are exact in it.
+ * integers up to 255 are exact in it.  Rows that others wrote may have any finite z,
+ * below 0, above the codes or not whole.
  *   k, v          device pointers, 16-byte aligned.  Row (page, head, t) starts at
  *                 byte page * page_stride + head * head_stride + t * token_stride;
  *                 the strides are not negative and multiples of 16, so [page][head][t]
@@ -520,7 +521,8 @@ fq_status fq_kv_cache_write(const fq_kv_cache* cache, const uint16_t* K, const u
  *   slots      device int64 [n_tokens], in any order, with repeats; a slot outside
  *              [0, n_pages * page_size) gives rows of zeros.
  *   K, V       device outputs [n_tokens][n_kv_heads][head_dim], contiguous, 16-byte
- *              aligned; dtype FQ_Y_BF16 (rounded to nearest even once) or FQ_Y_F32 (exact).
+ *              aligned; dtype FQ_Y_BF16 (rounded to nearest even once) or FQ_Y_F32 (exact
+ *              where c - z has up to 16 bits, as all that fq_kv_cache_write stores).
  * Errors: as fq_kv_cache_write.
  */
 fq_status fq_kv_cache_read(const fq_kv_cache* cache, const int64_t* slots, int64_t n_tokens,

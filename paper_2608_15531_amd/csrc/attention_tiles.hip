@@ -13,9 +13,13 @@
 // by 16 lanes).  bf16 rows go from memory straight to LDS, without a register.  Two tiles:
 // the next one is under way during a tile's products.
 //
-// Quantised caches become c - z on the way into LDS, which is exact in bf16 (|c - z| <=
-// 255); the rows' scales are applied in fp32, s_k to the scores and s_v to the weights
-// before these are rounded.
+// Quantised caches: the codes become bf16 on the way into LDS, exactly, and the affine map is
+// applied to the sums in fp32, as in the kernel for few rows, so that any zero-point counts
+// as it is (c - z of one above 255 or not whole does not fit a bf16):
+//     q . k = s_k (sum q c - z_k sum q),   sum p v = sum p' c - sum p' z_v,   p' = bf16(p s_v).
+// z_k sum q is one more product a 32 keys, with sum q as three bf16 that together are the
+// fp32 number (700 tokens over 2700 keys, 8 bits: 92 us; as 32 multiply-adds 95; 88 with
+// c - z formed in LDS, which holds whole z up to 255 only).
 //
 // 2048 tokens over 8192 keys, 32 heads on 8, D = 128, bf16: 263 to 293 us, 820 to 915
 // TFLOP/s (a product of 8192^3: 1213).  The matrix cores are busy 39 % of the time:
@@ -43,6 +47,10 @@ __device__ __forceinline__ f32x16_t mfma32(bf16x8_t a, bf16x8_t b, f32x16_t c) {
 __device__ __forceinline__ float pair_max(float v) { return across32(v, Max{}); }
 __device__ __forceinline__ float pair_add(float v) { return across32(v, Add{}); }
 
+__device__ __forceinline__ float upper_bf16(float v) {
+  return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v) & 0xFFFF0000u);
+}
+
 // Two f32 whose upper halves are exact bf16, as a pair.
 __device__ __forceinline__ uint32_t pack_exact(float lo, float hi) {
   return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
@@ -52,8 +60,8 @@ template <int D>
 struct TileLds {
   static constexpr int K = kTile * D * 2, V = K;
   static constexpr int kv = K + V;
-  static constexpr int scales = kTile * 4;          // bf16 s_k | bf16 s_v << 16
-  static constexpr int one = kv + scales;
+  static constexpr int meta = kTile * 4;            // of K, then of V: bf16 s | bf16 z << 16
+  static constexpr int one = kv + 2 * meta;
   static constexpr int bytes = 2 * one;
 };
 
@@ -145,11 +153,11 @@ struct Share {
     }
   }
 
-  // code j of words x, less the zero-point
+  // code j of words x
   template <int W>
-  __device__ static __forceinline__ float value(const uint32_t (&x)[W], int j, float z) {
-    if constexpr (KIND == FQ_KV_INT8) return float((x[j / 4] >> (8 * (j & 3))) & 255u) - z;
-    else return float((x[j / 8] >> (4 * (j & 7))) & 15u) - z;
+  __device__ static __forceinline__ float value(const uint32_t (&x)[W], int j) {
+    if constexpr (KIND == FQ_KV_INT8) return float((x[j / 4] >> (8 * (j & 3))) & 255u);
+    else return float((x[j / 8] >> (4 * (j & 7))) & 15u);
   }
 
   // Codes into a tile as bf16.
@@ -161,21 +169,20 @@ struct Share {
         const int idx = i * 256 + tid, row = idx / PPR, piece = idx % PPR;
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
-          // (a place that was never written can hold any bits: c - z stays finite there too,
-          // and the weight of a key that is not seen is 0)
-          const float z = fminf(fmaxf(__builtin_bit_cast(float, meta[v][i] & 0xFFFF0000u), 0.f), 255.f);
 #pragma unroll
           for (int c = 0; c < CH; ++c) {
             uint32_t o[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              o[e] = pack_exact(value(w[v][i], 8 * c + 2 * e, z), value(w[v][i], 8 * c + 2 * e + 1, z));
+              o[e] = pack_exact(value(w[v][i], 8 * c + 2 * e), value(w[v][i], 8 * c + 2 * e + 1));
             *reinterpret_cast<uint4*>(lds + v * TileLds<D>::K + row * 2 * D + ((piece * CH + c) ^ swizzle<D>(row)) * 16) =
                 uint4{o[0], o[1], o[2], o[3]};
           }
         }
-        if (piece == 0)
-          *reinterpret_cast<uint32_t*>(lds + TileLds<D>::kv + 4 * row) = (meta[0][i] & 0xFFFFu) | meta[1][i] << 16;
+        if (piece == 0) {
+          *reinterpret_cast<uint32_t*>(lds + TileLds<D>::kv + 4 * row) = meta[0][i];
+          *reinterpret_cast<uint32_t*>(lds + TileLds<D>::kv + TileLds<D>::meta + 4 * row) = meta[1][i];
+        }
       }
     }
   }
@@ -237,18 +244,32 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
   const bool use_q = mine.in && a.scale_log2 != 0.f;
   const uint16_t* qp = a.Q + (it.t0 + mine.token) * a.q_token + mine.head * a.q_head;
   bf16x8_t qv[STEPS];
+  float q_sum = 0.f;
 #pragma unroll
   for (int st = 0; st < STEPS; ++st) {
     uint4 w{0, 0, 0, 0};
     if (use_q) w = *reinterpret_cast<const uint4*>(qp + st * 16 + h * 8);
-    qv[st] = __builtin_bit_cast(bf16x8_t, u32x4_t{w.x ^ q_sign, w.y ^ q_sign, w.z ^ q_sign, w.w ^ q_sign});
+    const u32x4_t ws{w.x ^ q_sign, w.y ^ q_sign, w.z ^ q_sign, w.w ^ q_sign};
+    if constexpr (KIND != FQ_KV_BF16) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        q_sum += bf16_bits_to_f32(ws[i]) + __builtin_bit_cast(float, ws[i] & 0xFFFF0000u);
+    }
+    qv[st] = __builtin_bit_cast(bf16x8_t, ws);
+  }
+  // - sum q as three bf16, 8 bits each, against z, z, z
+  bf16x8_t zq;
+  if constexpr (KIND != FQ_KV_BF16) {
+    const float all = -pair_add(q_sum), hi = upper_bf16(all), mid = upper_bf16(all - hi), lo = all - hi - mid;
+    zq = __builtin_bit_cast(bf16x8_t, u32x4_t{pack_exact(hi, mid), pack_exact(lo, 0.f), 0u, 0u});
   }
   f32x16_t acc[DB];
 #pragma unroll
   for (int c = 0; c < DB; ++c)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
-  float m = kNegInf, l = 0.f;   // m in units of q.k, of this lane's row; l of this lane's keys
+  // m in units of q.k, of this lane's row; l and the sum of p' z_v of this lane's keys
+  float m = kNegInf, l = 0.f, corr = 0.f;
 
   const int32_t* table = a.table + it.seq * a.table_stride;
   const char* kh = a.k + it.head * a.head_stride;
@@ -318,6 +339,14 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int j = 0; j < 16; ++j) s[kb][j] = 0.f;
+      if constexpr (KIND != FQ_KV_BF16) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(lds + TileLds<D>::kv + 4 * (kb * 32 + r32));
+          const uint32_t z = h ? 0u : w >> 16;   // the other half of the operand's 16 places is 0
+          s[kb] = mfma32(__builtin_bit_cast(bf16x8_t, u32x4_t{z | z << 16, z, 0u, 0u}), zq, s[kb]);
+        }
+      }
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -330,10 +359,10 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             const uint4 w = *reinterpret_cast<const uint4*>(lds + TileLds<D>::kv + 4 * (kb * 32 + 8 * g + 4 * h));
-            s[kb][4 * g] *= bf16_bits_to_f32(w.x);
-            s[kb][4 * g + 1] *= bf16_bits_to_f32(w.y);
-            s[kb][4 * g + 2] *= bf16_bits_to_f32(w.z);
-            s[kb][4 * g + 3] *= bf16_bits_to_f32(w.w);
+            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              s[kb][4 * g + e] *= bf16_bits_to_f32(ws[e]);
           }
       }
       const bool whole = key0 + kTile - 1 <= wp_lo &&
@@ -368,6 +397,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
         const float shrink = __builtin_amdgcn_exp2f((m - (m_new == kNegInf ? 0.f : m_new)) * c2);
         m = m_new;
         l *= shrink;
+        if constexpr (KIND != FQ_KV_BF16) corr *= shrink;
 #pragma unroll
         for (int c = 0; c < DB; ++c) acc[c] *= shrink;
       }
@@ -381,21 +411,28 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
           p[e] = __builtin_amdgcn_exp2f(fmaf(s[kb][8 * (st & 1) + e], c2, base));
           l += p[e];
         }
+        uint32_t vmw[8];
         if constexpr (KIND != FQ_KV_BF16) {
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            const uint4 w = *reinterpret_cast<const uint4*>(lds + TileLds<D>::kv + 4 * (st * 16 + 8 * g + 4 * h));
+            const uint4 w = *reinterpret_cast<const uint4*>(lds + TileLds<D>::kv + TileLds<D>::meta +
+                                                            4 * (st * 16 + 8 * g + 4 * h));
             const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              float f = __builtin_bit_cast(float, ws[e] & 0xFFFF0000u);
-              if (!whole) f = (seen >> (st * 8 + 4 * g + e)) & 1u ? f : 0.f;   // whatever its scale
-              p[4 * g + e] *= f;
+              // a key that is not seen counts nothing, whatever its scale and zero-point
+              vmw[4 * g + e] = whole || ((seen >> (st * 8 + 4 * g + e)) & 1u) ? ws[e] : 0u;
+              p[4 * g + e] *= bf16_bits_to_f32(vmw[4 * g + e]);
             }
           }
         }
-        const bf16x8_t pb = __builtin_bit_cast(
-            bf16x8_t, u32x4_t{pk_bf16(p[0], p[1]), pk_bf16(p[2], p[3]), pk_bf16(p[4], p[5]), pk_bf16(p[6], p[7])});
+        const u32x4_t pw{pk_bf16(p[0], p[1]), pk_bf16(p[2], p[3]), pk_bf16(p[4], p[5]), pk_bf16(p[6], p[7])};
+        const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, pw);
+        if constexpr (KIND != FQ_KV_BF16) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            corr = dot2_bf16(pw[e], __builtin_amdgcn_perm(vmw[2 * e + 1], vmw[2 * e], 0x07060302u), corr);
+        }
 #pragma unroll
         for (int c = 0; c < DB; ++c) {
           const uint2 lo = read_transposed(v_at[c][0] + at + st * 16 * 2 * D);
@@ -403,7 +440,9 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
           acc[c] = mfma32(__builtin_bit_cast(bf16x8_t, u32x4_t{lo.x, lo.y, hi.x, hi.y}), pb, acc[c]);
         }
       }
-      order_products<4 * DB, 2, 4, 28, 7>();
+      // (with codes there are twice as many vector operations, which this order holds back:
+      // 700 tokens over 2700 keys, 8 bits, 97 us with it)
+      if constexpr (KIND == FQ_KV_BF16) order_products<4 * DB, 2, 4, 28, 7>();
     }
     if (more) {
       share.store(tile_lds + (buf ^ 1) * TileLds<D>::one, tid);
@@ -426,6 +465,11 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
   }
   // lane (r32, h) has channels 32 c + 8 (i / 4) + 4 h + i % 4 of its row
   l = pair_add(l);
+  if constexpr (KIND != FQ_KV_BF16) {
+    corr = pair_add(corr);
+#pragma unroll
+    for (int c = 0; c < DB; ++c) acc[c] -= corr;
+  }
   if (it.n_parts > 1) {
     // partial sums for join_kernel: [item][range][row][D + 4] floats, the last four: m c2, l
     const int64_t item = it.number;

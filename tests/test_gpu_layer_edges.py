@@ -1,0 +1,87 @@
+"""The cache and attention on the GPU where contents or arguments are unusual, against the
+float64 oracle.
+
+Tolerances, elementwise, from the formats and the order of the operations:
+* One rounding to bf16: 2^-9 of the value; the softmax weights (times V's scale) are rounded
+  so too, which moves a row by 2^-9 sum w |v| at most.
+* Scores: fp32 sums of D products and, with codes, of D numbers times the zero-point, of
+  magnitude |q| s (c + |z|) (4 bits: 16 + c in one kernel), each addition off by 2^-23 at most
+  (the matrix instructions need not round to nearest); d of the row's largest such sum moves
+  a weight by a factor of up to e^(2 d), and with it a row by 2.5 d sum w |v|.
+* The sums of n weights times codes: n additions of magnitude max s (c + |z|) at most, 2^-23 each.
+* The log-sum: d, and 2^-20 of it and of 1 for the exponentials and the logarithm.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer as L
+from test_gpu_layer import Step, codes_of, f64, log, tiles_bounds
+
+pytestmark = pytest.mark.gpu
+
+
+def check_rows(out, lse, q, cu, held, size, q_lens, kv_lens, D, scale, window=0, sinks=0, every=1):
+    """out, lse of each sequence's every `every`-th token against attention over `held`
+    (K, V by sequence, [keys][heads][D]), whose summands have the magnitudes `size`."""
+    out, lse, q = f64(out), f64(lse), f64(q)
+    hq, hkv = q.shape[1], held[0][0].shape[1]
+    G = hq // hkv
+    for b, (n, S) in enumerate(zip(q_lens, kv_lens)):
+        for i in sorted(set(range(0, n, every)) | {n - 1}):
+            see = L.visible(S - n + i, S, window, sinks)
+            t = cu[b] + i
+            for h in range(hq):
+                K, V = (held[x][b][:, h // G] for x in (0, 1))
+                o, e, A, _ = L.attention_row(q[t, h], K, V, see, scale)
+                where = f"sequence {b} token {i} head {h}"
+                if not see.any():
+                    assert (out[t, h] == 0).all() and lse[t, h] == -np.inf, where
+                    continue
+                d = 2 * (D + 8) * 2.0 ** -23 * abs(scale) * (size[0][b][see, h // G] @ np.abs(q[t, h])).max()
+                tol = 2.0 ** -9 * 1.01 * np.abs(o) + (2.0 ** -9 * 1.01 + 2.5 * d) * A + \
+                    see.sum() * 2.0 ** -23 * size[1][b][see, h // G].max(0) + 1e-30
+                err = np.abs(out[t, h] - o)
+                assert (err <= tol).all(), (where, float((err - tol).max()), np.flatnonzero(~(err <= tol))[:4])
+                assert abs(lse[t, h] - e) <= d + 2.0 ** -20 * (1 + abs(e)), (where, lse[t, h], e)
+
+
+def held_codes(st):
+    """(K, V) that the step's cache holds by sequence, and the magnitudes of their summands."""
+    held, size = ([], []), ([], [])
+    page = st.cache.page_size
+    for b, n in enumerate(st.kv_lens):
+        t = torch.arange(n)
+        slots = st.table[b].long()[t // page] * page + t % page
+        for x, (c, s, z) in enumerate(codes_of(st.cache, slots)):
+            held[x].append(s * (c - z))
+            size[x].append(np.abs(s) * (c + np.abs(z) + (16 if st.kind == "int4" else 0)))
+    return held, size
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kind", ["int8", "int4"])
+@pytest.mark.parametrize("q_lens,kv_lens,window", [([3, 1], [120, 77], 0), ([70, 9], [330, 20], 0), ([70], [330], 40),
+                                                   ([30], [2100], 0)],
+                         ids=["rows", "tiles", "tiles_window", "tiles_split"])
+def test_attention_over_any_zero_points(gpu_lib, q_lens, kv_lens, window, kind, D):
+    """A row stands for s (c - z) with any bf16 z: below 0, above the codes, not whole."""
+    fq = gpu_lib
+    hq, hkv, page = 4, 2, 16
+    st = Step(fq, kind, D, hq, hkv, page, q_lens, kv_lens, seed=31 + D)
+    g = torch.Generator().manual_seed(5)
+    values = torch.tensor([-3.0, 12.5, 300.0, -0.25, 0.0, 7.75, 255.0, -120.0]).to(torch.bfloat16).cuda()
+    for b, n in enumerate(kv_lens):
+        t = torch.arange(n)
+        at, off = st.table[b].long()[t // page].cuda(), (t % page).cuda()
+        for meta in (st.cache.k_meta, st.cache.v_meta):
+            meta[at, :, off, 1] = values[torch.randint(0, 8, (n, hkv), generator=g).cuda()]
+    if q_lens[0] > 3:
+        c = tiles_bounds(st, window, by_keys=kv_lens[0] > 2000)
+        assert c["kernel"] == "tiles" and (c["split"] > 1 or kv_lens[0] < 2000)
+    log(f"attention zero-points {kind} D={D} {q_lens} {kv_lens} window {window}")
+    out, lse = fq.fq_paged_attention(st.q, st.cache, st.batch, window=window, return_lse=True)
+    torch.cuda.synchronize()
+    held, size = held_codes(st)
+    check_rows(out, lse, st.q, st.cu, held, size, q_lens, kv_lens, D, float(np.float32(D ** -0.5)), window, every=5)
