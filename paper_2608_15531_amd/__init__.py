@@ -23,6 +23,7 @@ LIB_PATH = os.path.join(_HERE, "libfq.so")
 
 FQ_OK = 0
 _FQ_ERR_WORKSPACE = 8
+_FQ_ERR_HIP = 9
 STATUS_NAMES = {0: "FQ_OK", 1: "FQ_ERR_NULL", 2: "FQ_ERR_SHAPE", 3: "FQ_ERR_RANGE",
                 4: "FQ_ERR_DUPLICATE", 5: "FQ_ERR_ZERO_VALUE", 6: "FQ_ERR_FORMAT",
                 7: "FQ_ERR_UNSUPPORTED", 8: "FQ_ERR_WORKSPACE", 9: "FQ_ERR_HIP",
@@ -399,6 +400,8 @@ class TileCOODevice:
 
 
 _workspaces: dict = {}
+_captured: dict = {}       # of graphs: (capture, workspace) by stream, the last capture only
+_COUNTER_BYTES = 256 * 1024   # of a workspace, which have to be zero before its first use
 
 
 def _stream_handle(stream, device) -> int:
@@ -424,16 +427,46 @@ def _stream_of(stream, index: int) -> int:
     return _raw_stream(index)
 
 
-def workspace(nbytes: int, device, stream_handle: int):
+def _capture_of(stream, stream_handle: int):
+    """Number of the graph capture that the stream is part of, or None."""
+    if stream is None and not _torch().cuda.is_current_stream_capturing():
+        return None
+    if not stream_handle:
+        return None   # the default stream cannot be captured
+    status, number = C.c_int(0), C.c_ulonglong(0)
+    if load().hipStreamGetCaptureInfo(C.c_void_p(stream_handle), C.byref(status), C.byref(number)):
+        raise FqError(_FQ_ERR_HIP, "hipStreamGetCaptureInfo")
+    return number.value if status.value else None
+
+
+def _kept(key, capture):
+    """The workspace kept for (device index, stream), in a capture that of the capture."""
+    if capture is None:
+        return _workspaces.get(key)
+    number, buf = _captured.get(key, (None, None))
+    return buf if number == capture else None
+
+
+def workspace(nbytes: int, device, stream_handle: int, capture=None):
     """Zero-filled workspace kept per (device, stream); the kernels leave it zeroed.
     Call it with the kernel's stream current (see _on_stream): the allocation
-    and its zero fill are then ordered before the kernel on that stream."""
+    and its zero fill are then ordered before the kernel on that stream.
+
+    capture: number of the graph capture that the call is recorded in (_capture_of).  The
+    workspace then comes from the graph's memory, no eager call and no other graph uses it,
+    and its counters' zero fill is recorded with it, so each replay starts with it: a kept
+    one may be gone when the graph is replayed, or never have been cleared."""
     torch = _torch()
     key = (torch.device(device).index, stream_handle)
-    buf = _workspaces.get(key)
+    buf = _kept(key, capture)
     if buf is None or buf.numel() < nbytes:
-        buf = torch.zeros(max(nbytes, 256), dtype=torch.uint8, device=device)
-        _workspaces[key] = buf
+        if capture is None:
+            buf = torch.zeros(max(nbytes, 256), dtype=torch.uint8, device=device)
+            _workspaces[key] = buf
+        else:
+            buf = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+            buf[:_COUNTER_BYTES].zero_()
+            _captured[key] = (capture, buf)
     return buf
 
 
@@ -457,10 +490,12 @@ def _launch(call, sizer, pr, ws, device, stream, where):
     fails (or none is kept yet) is the size asked for and a larger one made.  With
     more than 16 rows the size is always asked for: there a smaller workspace may
     pass the check and get the strip kernel in the row-block kernel's place, so the
-    kernel would depend on the calls before."""
+    kernel would depend on the calls before.  Calls recorded in a graph share one of the
+    graph's own (workspace)."""
     sh = _stream_handle(stream, device)
     if ws is None:
-        ws = _workspaces.get((device.index, sh)) if pr.M <= _STRIP_ROWS else None
+        capture = _capture_of(stream, sh)
+        ws = _kept((device.index, sh), capture) if pr.M <= _STRIP_ROWS else None
         if ws is not None:
             status = call(ws, sh)
             if status != _FQ_ERR_WORKSPACE:
@@ -469,7 +504,7 @@ def _launch(call, sizer, pr, ws, device, stream, where):
         need = C.c_size_t(0)
         _check(sizer(C.byref(pr), C.byref(need)), sizer.__name__)
         with _on_stream(stream):
-            ws = workspace(need.value, device, sh)
+            ws = workspace(need.value, device, sh, capture)
     _check(call(ws, sh), where)
 
 
@@ -773,7 +808,7 @@ class PagedBatch:
     kv_lens int32 [n_seqs] (tokens in the cache, the new ones included), block_table
     int32 [n_seqs][pages], and upper bounds max_q and max_kv of the new tokens and of
     kv_lens.  Made once for all layers of a step; the tensors' contents may change
-    between calls within the bounds (as under graph replay)."""
+    between calls, and between replays of a graph, within the bounds."""
 
     def __init__(self, cu_q, kv_lens, block_table, max_q: int, max_kv: int):
         torch = _torch()
@@ -858,7 +893,12 @@ def fq_paged_attention(q, cache: KVCache, batch: PagedBatch, scale: float | None
     first `sinks` keys.  Returns out (bf16, like q), and with return_lse also the ln of
     the softmax sums, fp32 [total_q][n_heads].  A token that sees no key gets zeros and
     -infinity; rows of q that belong to no sequence are left as they are in `out`
-    (unspecified in a new one)."""
+    (unspecified in a new one).
+
+    ws: a zero-filled uint8 workspace of fq_paged_attention_workspace_bytes or more, for calls
+    that do not overlap in time.  Without one the workspace kept for the stream is used, which
+    grows to the largest call's (277 MB of partial sums at most) and is not given back; a
+    call recorded in a graph uses one in the graph's memory."""
     torch = _torch()
     lib = load()
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
@@ -884,7 +924,8 @@ def fq_paged_attention(q, cache: KVCache, batch: PagedBatch, scale: float | None
     sh = _stream_of(stream, index)
     pq, po = q.data_ptr(), out.data_ptr()
     pl = None if lse is None else lse.data_ptr()
-    w = _workspaces.get((index, sh)) if ws is None else ws
+    capture = _capture_of(stream, sh) if ws is None else None
+    w = _kept((index, sh), capture) if ws is None else ws
     status = lib.fq_paged_attention(ref, pq, cache._ref, cu, lens, table, po, pl,
                                     None if w is None else w.data_ptr(),
                                     0 if w is None else w.numel(), sh)
@@ -894,7 +935,7 @@ def fq_paged_attention(q, cache: KVCache, batch: PagedBatch, scale: float | None
         _check(lib.fq_paged_attention_workspace_bytes(ref, cache._ref, C.byref(need)),
                "fq_paged_attention_workspace_bytes")
         with _on_stream(stream):
-            w = workspace(need.value, cache.device, sh)
+            w = workspace(need.value, cache.device, sh, capture)
         status = lib.fq_paged_attention(ref, pq, cache._ref, cu, lens, table, po, pl,
                                         w.data_ptr(), w.numel(), sh)
     if status:
