@@ -185,6 +185,11 @@ struct Row {
 
 constexpr float kNegInf = -__builtin_inff();
 
+// By how much a score (before the factor c2 > 0) may pass the running maximum until the sums
+// move to it: 2^8 in weights.  Finite for the smallest c2 too: -infinity, the first maximum,
+// plus an infinity would be no number, and no score would pass it.
+__device__ __forceinline__ float grow_of(float c2) { return fminf(8.f / c2, 3.402823466e38f); }
+
 // Infinities and NaN of a bf16 V row that some rows of a block see and others do not: in
 // the matrix product their zero weights would make NaN of them.  So in tiles that are not
 // seen whole, V's values that are not finite enter the product as 0, and where there were

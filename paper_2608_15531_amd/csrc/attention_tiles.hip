@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
   // softmax in powers of two of |scale|; a negative scale changes the sign of q, 0 makes it 0
   const uint32_t q_sign = a.scale_log2 < 0.f ? 0x80008000u : 0u;
   const float c2 = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
-  const float grow = 8.f / c2;
+  const float grow = grow_of(c2);
   const bool use_q = mine.in && a.scale_log2 != 0.f;
   const uint16_t* qp = a.Q + (it.t0 + mine.token) * a.q_token + mine.head * a.q_head;
   bf16x8_t qv[STEPS];

@@ -85,3 +85,25 @@ def test_attention_over_any_zero_points(gpu_lib, q_lens, kv_lens, window, kind, 
     torch.cuda.synchronize()
     held, size = held_codes(st)
     check_rows(out, lse, st.q, st.cu, held, size, q_lens, kv_lens, D, float(np.float32(D ** -0.5)), window, every=5)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8", "int4"])
+@pytest.mark.parametrize("q_lens,kv_lens", [([2, 1], [300, 40]), ([60], [140]), ([60], [2500])],
+                         ids=["rows", "tiles", "tiles_split"])
+@pytest.mark.parametrize("scale", [1.5e-38, 1e-38, -1e-40, 1e-45])
+def test_attention_smallest_scales(gpu_lib, scale, q_lens, kv_lens, kind):
+    """Scales whose inverse is beyond fp32: the mean of the values, ln of the keys."""
+    fq = gpu_lib
+    st = Step(fq, kind, 128, 4, 2, 16, q_lens, kv_lens, seed=19)
+    if len(q_lens) == 1:
+        c = tiles_bounds(st, by_keys=kv_lens[0] > 2000)
+        assert c["split"] > 1 or kv_lens[0] < 2000
+    log(f"attention scale {scale} {kind} {kv_lens}")
+    out, lse = fq.fq_paged_attention(st.q, st.cache, st.batch, scale=scale, return_lse=True)
+    torch.cuda.synchronize()
+    if kind == "bf16":
+        held = [[f64(t) for t in ts] for ts in (st.k, st.v)]
+        size = [[np.abs(t) for t in ts] for ts in held]
+    else:
+        held, size = held_codes(st)
+    check_rows(out, lse, st.q, st.cu, held, size, q_lens, kv_lens, 128, float(np.float32(scale)), every=13)
