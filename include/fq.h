@@ -545,7 +545,7 @@ fq_status fq_kv_cache_read(const fq_kv_cache* cache, const int64_t* slots, int64
  *   window      0: every token sees the keys up to its own.  W > 0: only the last W of
  *               them (its own included) and the first `sinks` keys of the sequence.
  *   sinks       >= 0; without a window it changes nothing.
- *   scale       factor of q.k, finite.
+ *   scale       factor of q.k; finite, also times log2(e) (|scale| up to 2.358e38).
  *   strides     of Q and O, in elements, multiples of 8; block_table rows have
  *               table_cols entries, table_stride apart.
  * The new token i of a sequence stands at position p = kv_lens - q_len + i and sees key j

@@ -619,7 +619,7 @@ int launch_attention(const AttnPlan& pl, const fq_attention& a, const fq_kv_cach
   g.split_tiles = pl.split_tiles;
   g.part_rows = pl.part_rows;
   g.dense_blocks = pl.dense_blocks;
-  g.scale_log2 = a.scale * 1.44269504088896340736f;
+  g.scale_log2 = a.scale * kLog2e;
   const dim3 grid(unsigned(int64_t(pl.row_blocks) * pl.split * c.n_kv_heads), unsigned(a.n_seqs));
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (pl.kernel == FQ_ATTN_TILES) return fqk::launch_attn_tiles(g, c.kind, c.head_dim, grid, s);

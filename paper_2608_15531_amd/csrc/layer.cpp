@@ -62,7 +62,8 @@ fq_status check_attention(const fq_attention* a, const fq_kv_cache* c) {
     return FQ_ERR_SHAPE;
   if (a->n_heads % c->n_kv_heads != 0) return FQ_ERR_SHAPE;
   if (int64_t(a->table_cols) * c->page_size < a->max_kv) return FQ_ERR_SHAPE;
-  if (!std::isfinite(a->scale)) return FQ_ERR_SHAPE;
+  // (the softmax runs in powers of two)
+  if (!std::isfinite(a->scale * fqi::kLog2e)) return FQ_ERR_SHAPE;
   const int64_t strides[4] = {used(a->q_token_stride, a->total_q), used(a->q_head_stride, a->n_heads),
                               used(a->o_token_stride, a->total_q), used(a->o_head_stride, a->n_heads)};
   for (int64_t s : strides)

@@ -16,6 +16,7 @@ constexpr int kKvTile = 2 * kKvBlock;
 // Rows and keys of a workgroup's tile in the kernel for many rows.
 constexpr int kTilesRows = 128;
 constexpr int kTilesKeys = 64;
+constexpr float kLog2e = 1.44269504088896340736f;
 
 // Launch plan of one attention call, from the sizes alone.
 struct AttnPlan {

@@ -310,3 +310,11 @@ def test_oracle_norm_closed_forms():
     np.testing.assert_allclose(h[0], np.array([6.0, 1.5]) / np.sqrt((9 + 2.25) / 2))
     r, h, _ = L.gated_residual_norm(x, None, None, None, None, 1.0, 1e-5)
     assert (r == x).all() and h is None
+
+
+@pytest.mark.parametrize("scale,want", [(2.358e38, "FQ_OK"), (-2.358e38, "FQ_OK"), (2.36e38, "FQ_ERR_SHAPE"),
+                                        (-3.4e38, "FQ_ERR_SHAPE")])
+def test_attention_scales_beyond_its_powers_of_two(lib, scale, want):
+    """The kernels multiply by scale log2(e), which has to be finite too."""
+    c, a, n = cache(), attn(scale=scale), C.c_size_t(7)
+    assert name(lib.fq_paged_attention_workspace_bytes(C.byref(a), C.byref(c), C.byref(n))) == want
