@@ -551,6 +551,8 @@ fq_status fq_kv_cache_read(const fq_kv_cache* cache, const int64_t* slots, int64
  * The new token i of a sequence stands at position p = kv_lens - q_len + i and sees key j
  * iff j <= p and (window == 0 or j > p - window or j < sinks).  With p < 0 it sees none:
  * its output row is 0 and its lse -infinity.  So it is too where every score is -infinity.
+ * Where scale log2(e) q.k of its largest score is beyond fp32, a row and its lse are NaN;
+ * where that of another seen key is, they may be.
  * A key that a token does not see cannot change its row, whatever the cache holds there
  * (infinities and NaN too).
  */

@@ -486,19 +486,21 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) attn_tiles_kernel(AttnArgs
   }
   m *= c2;
   if (!mine.in) return;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  // (with a maximum beyond fp32 every weight came out as 0 as well: such a row is NaN)
+  const bool none = l == 0.f && m == kNegInf;
+  const float inv = 1.f / l;
   uint16_t* op = a.O + (it.t0 + mine.token) * a.o_token + mine.head * a.o_head;
 #pragma unroll
   for (int c = 0; c < DB; ++c)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       uint2 w{0, 0};
-      if (l != 0.f)
+      if (!none)
         w = uint2{pk_bf16(acc[c][4 * g] * inv, acc[c][4 * g + 1] * inv), pk_bf16(acc[c][4 * g + 2] * inv, acc[c][4 * g + 3] * inv)};
       *reinterpret_cast<uint2*>(op + 32 * c + 8 * g + 4 * h) = w;
     }
   if (a.lse && h == 0)
-    a.lse[(it.t0 + mine.token) * a.n_heads + mine.head] = l == 0.f ? kNegInf : (m + __log2f(l)) * 0.69314718055994530942f;
+    a.lse[(it.t0 + mine.token) * a.n_heads + mine.head] = none ? kNegInf : (m + __log2f(l)) * 0.69314718055994530942f;
 }
 
 // Joins the ranges of rows whose keys were split, in their order: D / 8 threads a row,

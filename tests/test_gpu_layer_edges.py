@@ -107,3 +107,25 @@ def test_attention_smallest_scales(gpu_lib, scale, q_lens, kv_lens, kind):
     else:
         held, size = held_codes(st)
     check_rows(out, lse, st.q, st.cu, held, size, q_lens, kv_lens, 128, float(np.float32(scale)), every=13)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8", "int4"])
+@pytest.mark.parametrize("scale", [1e38, -1e38])
+@pytest.mark.parametrize("q_lens,kv_lens", [([2, 1], [300, 40]), ([60], [140]), ([60], [2500])],
+                         ids=["rows", "tiles", "tiles_split"])
+def test_attention_scores_beyond_fp32(gpu_lib, q_lens, kv_lens, scale, kind):
+    """128 scale is no fp32 number: the rows are NaN, not zeros."""
+    fq = gpu_lib
+
+    def edit(b, k, v):
+        k[:] = 1.0
+
+    st = Step(fq, kind, 128, 4, 2, 16, q_lens, kv_lens, seed=23, edit=edit)
+    st.q.fill_(1.0)
+    if len(q_lens) == 1:
+        c = tiles_bounds(st, by_keys=kv_lens[0] > 2000)
+        assert c["split"] > 1 or kv_lens[0] < 2000
+    log(f"attention scores beyond fp32 {kind} {kv_lens} {scale}")
+    out, lse = fq.fq_paged_attention(st.q, st.cache, st.batch, scale=scale, return_lse=True)
+    torch.cuda.synchronize()
+    assert torch.isnan(out).all() and torch.isnan(lse).all()
