@@ -876,8 +876,9 @@ def fq_kv_cache_read(cache: KVCache, slots, k=None, v=None, dtype="bf16", stream
 
 def _attention(n_heads, q_strides, o_strides, total_q, cache, batch, scale, window, sinks):
     # ctypes would cut wider numbers to 32 bits
-    if max(batch.max_q, batch.max_kv, window, sinks) > 0x7FFFFFFF:
-        raise ValueError("max_q, max_kv, window and sinks: below 2^31")
+    numbers = (batch.max_q, batch.max_kv, window, sinks)
+    if max(numbers) > 0x7FFFFFFF or min(numbers) < -0x80000000:
+        raise ValueError("max_q, max_kv, window and sinks: below 2^31, and not negative")
     return fq_attention(batch.n_seqs, n_heads, batch.max_q, batch.max_kv, window, sinks, total_q,
                         q_strides[0], q_strides[1], o_strides[0], o_strides[1],
                         batch.table_stride, batch._table_cols,

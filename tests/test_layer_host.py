@@ -318,3 +318,20 @@ def test_attention_scales_beyond_its_powers_of_two(lib, scale, want):
     """The kernels multiply by scale log2(e), which has to be finite too."""
     c, a, n = cache(), attn(scale=scale), C.c_size_t(7)
     assert name(lib.fq_paged_attention_workspace_bytes(C.byref(a), C.byref(c), C.byref(n))) == want
+
+
+@pytest.mark.parametrize("name", ["max_q", "max_kv", "window", "sinks"])
+@pytest.mark.parametrize("value", [-2**31 - 1, -2**32 + 5])
+def test_numbers_below_32_bits_are_refused(name, value):
+    """Which 32 bits would make positive; other negative ones reach the library's check."""
+    from types import SimpleNamespace
+
+    def call(value):
+        v = {**dict(max_q=1, max_kv=500, window=0, sinks=0), name: value}
+        batch = SimpleNamespace(n_seqs=1, max_q=v["max_q"], max_kv=v["max_kv"], table_stride=10, _table_cols=10)
+        return fq._attention(8, (1024, 128), (1024, 128), 1, SimpleNamespace(head_dim=128), batch, None, v["window"],
+                             v["sinks"])
+
+    with pytest.raises(ValueError):
+        call(value)
+    assert getattr(call(-1), name) == -1
