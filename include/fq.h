@@ -555,6 +555,9 @@ fq_status fq_kv_cache_read(const fq_kv_cache* cache, const int64_t* slots, int64
  * where that of another seen key is, they may be.
  * A key that a token does not see cannot change its row, whatever the cache holds there
  * (infinities and NaN too).
+ * An infinity or a NaN in V under a seen key makes that channel of the row an infinity or a
+ * NaN (with codes all of its channels NaN); a NaN also in an infinity's place where the
+ * key's weight is too small for fp32, which may depend on max_q and max_kv.
  */
 typedef struct {
   int32_t n_seqs;

@@ -193,8 +193,10 @@ __device__ __forceinline__ float grow_of(float c2) { return fminf(8.f / c2, 3.40
 // Infinities and NaN of a bf16 V row that some rows of a block see and others do not: in
 // the matrix product their zero weights would make NaN of them.  So in tiles that are not
 // seen whole, V's values that are not finite enter the product as 0, and where there were
-// any, a second walk over those tiles adds them to the rows that do see them (every weight
-// is positive, so the value itself, an infinity or a NaN, is what the sum becomes).
+// any, a second walk over those tiles adds them to the rows that do see them: times a
+// positive weight, an infinity or a NaN is itself.  A weight too small for fp32 is 0, and makes
+// a NaN of an infinity in the product of a whole tile and where sums are moved or joined by
+// it, but not in this walk: the channel is not finite either way, and no more is promised.
 __device__ __forceinline__ bool nonfinite_pair(uint32_t w) {
   return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
 }

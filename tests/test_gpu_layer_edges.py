@@ -129,3 +129,42 @@ def test_attention_scores_beyond_fp32(gpu_lib, q_lens, kv_lens, scale, kind):
     out, lse = fq.fq_paged_attention(st.q, st.cache, st.batch, scale=scale, return_lse=True)
     torch.cuda.synchronize()
     assert torch.isnan(out).all() and torch.isnan(lse).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+@pytest.mark.parametrize("tiles", [False, True], ids=["rows", "tiles"])
+@pytest.mark.parametrize("at", [3, 70, 137], ids=["whole", "whole_later", "partial"])
+def test_attention_infinities_of_no_weight(gpu_lib, at, tiles, kind):
+    """V holds an infinity under a seen key whose weight is far below fp32: that channel (with
+    codes, the row) is not finite, wherever the key lies, and the others are as without it."""
+    fq = gpu_lib
+    S, n = 140, 4   # tokens at 136 .. 139
+
+    def edit(bad):
+        def f(b, k, v):
+            k[:] = 1.0
+            k[at] = -1.0
+            if bad:
+                v[at, :, 7] = float("inf")
+                v[at, :, 9] = float("-inf")
+        return f
+
+    outs = []
+    for bad in (True, False):
+        st = Step(fq, kind, 128, 4, 2, 16, [n], [S], seed=27, edit=edit(bad))
+        st.q.fill_(3.0)
+        if tiles:
+            tiles_bounds(st)
+        log(f"attention infinity of no weight {kind} at {at} tiles={tiles} bad={bad}")
+        out, lse = fq.fq_paged_attention(st.q, st.cache, st.batch, scale=1.0, return_lse=True)   # scores of +-384
+        torch.cuda.synchronize()
+        outs.append((out, lse))
+    (out, lse), (clean, clean_lse) = outs
+    first = max(0, at - (S - n))   # the first token that sees it
+    assert torch.equal(out[:first], clean[:first]) and torch.equal(lse, clean_lse)
+    if kind == "bf16":
+        assert not torch.isfinite(out[first:, :, [7, 9]]).any()
+        keep = [c for c in range(128) if c not in (7, 9)]
+        assert torch.equal(out[:, :, keep], clean[:, :, keep])
+    else:
+        assert torch.isnan(out[first:]).all()
