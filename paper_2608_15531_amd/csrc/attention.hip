@@ -530,7 +530,7 @@ bool plan_attention(const fq_attention& a, const fq_kv_cache& c, AttnPlan* pl) {
   int64_t blocks = row_blocks * a.n_seqs;
   pl->dense_blocks = 0;
   if (pl->kernel == FQ_ATTN_TILES && a.total_q / pl->rows < blocks) {
-    const int64_t dense = a.total_q * group / pl->rows + a.n_seqs;
+    const int64_t dense = dense_blocks(a.total_q, group, pl->rows, a.n_seqs);
     if (dense < blocks) {
       blocks = dense;
       pl->dense_blocks = 1;

@@ -6,6 +6,7 @@
 
 #include <climits>
 
+#include "blocks.hpp"
 #include "device.hpp"
 #include "internal.hpp"
 #include "lanes.hpp"
@@ -15,6 +16,7 @@ namespace fqk {
 
 using fqi::kKvBlock;
 using fqi::kKvTile;
+using fqi::TileRange;
 
 struct AttnArgs {
   const uint16_t* Q;
@@ -69,30 +71,6 @@ __device__ __forceinline__ BlockPlace block_place(const AttnArgs& a, const int32
   return BlockPlace{min(page, a.n_pages - 1), (blk - col * a.page_blocks) * kKvBlock};
 }
 
-// Which tiles a block of rows at positions [p_lo, p_hi] sees: with a window, the tiles of
-// the first keys and those of the window, numbered one after the other.
-struct TileRange {
-  int first;   // tiles of the first keys
-  int skip;    // tiles between those and the window
-  int n;
-  __device__ __forceinline__ int tile(int i) const { return i < first ? i : i + skip; }
-};
-
-template <int TILE>
-__device__ __forceinline__ TileRange tile_range(int p_lo, int p_hi, int window, int sinks) {
-  TileRange r;
-  const int end = p_hi < 0 ? 0 : p_hi / TILE + 1;   // p_hi is the last key seen
-  r.first = 0;
-  r.skip = 0;
-  if (window > 0 && p_lo >= window) {
-    const int lo = (p_lo - window + 1) / TILE;
-    r.first = min(lo, (min(sinks, p_lo + 1) + TILE - 1) / TILE);
-    r.skip = lo - r.first;
-  }
-  r.n = max(0, end - r.skip);
-  return r;
-}
-
 // What a workgroup works on: a block of ROWS rows of one (sequence, KV head), one range of
 // the key tiles that the block sees.
 //
@@ -130,19 +108,18 @@ struct Item {
     rows = int(min(n_rows - row0, uint32_t(ROWS)));
     const int tok_lo = int(row0 / group);
     tok_hi = int((row0 + rows - 1) / group);
-    // by the rows before: a sequence whose rows are r .. s - 1 has at most as many blocks as
-    // s / ROWS - r / ROWS + 1
-    number = ((a.dense_blocks ? t0 * a.group / ROWS + seq : int64_t(seq) * a.row_blocks) + rb) * a.n_kv_heads + head;
+    number = (a.dense_blocks ? fqi::dense_number(t0, a.group, ROWS, seq, rb) : int64_t(seq) * a.row_blocks + rb) *
+                 a.n_kv_heads + head;
     p0 = kv_len - q_all;
     kv_seen = min(kv_len, a.max_kv);
     p_lo = min(p0 + tok_lo, kv_seen - 1);
     p_hi = min(p0 + tok_hi, kv_seen - 1);
-    tr = tile_range<TILE>(p_lo, p_hi, a.window, a.sinks);
+    tr = fqi::tile_range<TILE>(p_lo, p_hi, a.window, a.sinks);
     return true;
   }
   // how many ranges its tiles fall into
   __device__ __forceinline__ int parts(const AttnArgs& a) const {
-    return min(max(1, (tr.n + a.split_tiles - 1) / a.split_tiles), a.split);
+    return fqi::range_count(tr.n, a.split_tiles, a.split);
   }
   // What this workgroup works on; false: nothing.
   template <int ROWS, int TILE>
