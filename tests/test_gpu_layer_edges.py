@@ -2,8 +2,8 @@
 float64 oracle.
 
 Tolerances, elementwise, from the formats and the order of the operations:
-* One rounding to bf16: 2^-9 of the value; the softmax weights (times V's scale) are rounded
-  so too, which moves a row by 2^-9 sum w |v| at most.
+* One rounding to bf16: 2^-8 of the value (7 bits follow the leading one); the softmax weights
+  (times V's scale) are rounded so too, which moves a row by 2^-8 sum w |v| at most.
 * Scores: fp32 sums of D products and, with codes, of D numbers times the zero-point, of
   magnitude |q| s (c + |z|) (4 bits: 16 + c in one kernel), each addition off by 2^-23 at most
   (the matrix instructions need not round to nearest); d of the row's largest such sum moves
@@ -17,19 +17,20 @@ import pytest
 import torch
 
 from oracle import layer as L
-from test_gpu_layer import Step, codes_of, f64, log, tiles_bounds
+from test_gpu_layer import MANY, STEPS, Step, codes_of, f64, log, tiles_bounds
 
 pytestmark = pytest.mark.gpu
 
 
-def check_rows(out, lse, q, cu, held, size, q_lens, kv_lens, D, scale, window=0, sinks=0, every=1):
+def check_rows(out, lse, q, cu, held, size, q_lens, kv_lens, D, scale, window=0, sinks=0, every=1, unit=2 * 2.0 ** -23):
     """out, lse of each sequence's every `every`-th token against attention over `held`
-    (K, V by sequence, [keys][heads][D]), whose summands have the magnitudes `size`."""
+    (K, V by sequence, [keys][heads][D]), whose summands have the magnitudes `size`; unit: what
+    one addition of a score is off by."""
     out, lse, q = f64(out), f64(lse), f64(q)
     hq, hkv = q.shape[1], held[0][0].shape[1]
     G = hq // hkv
     for b, (n, S) in enumerate(zip(q_lens, kv_lens)):
-        for i in sorted(set(range(0, n, every)) | {n - 1}):
+        for i in sorted(set(range(0, n, every)) | set(range(n)[-1:])):
             see = L.visible(S - n + i, S, window, sinks)
             t = cu[b] + i
             for h in range(hq):
@@ -39,8 +40,8 @@ def check_rows(out, lse, q, cu, held, size, q_lens, kv_lens, D, scale, window=0,
                 if not see.any():
                     assert (out[t, h] == 0).all() and lse[t, h] == -np.inf, where
                     continue
-                d = 2 * (D + 8) * 2.0 ** -23 * abs(scale) * (size[0][b][see, h // G] @ np.abs(q[t, h])).max()
-                tol = 2.0 ** -9 * 1.01 * np.abs(o) + (2.0 ** -9 * 1.01 + 2.5 * d) * A + \
+                d = (D + 8) * unit * abs(scale) * (size[0][b][see, h // G] @ np.abs(q[t, h])).max()
+                tol = 2.0 ** -8 * 1.01 * np.abs(o) + (2.0 ** -8 * 1.01 + 2.5 * d) * A + \
                     see.sum() * 2.0 ** -23 * size[1][b][see, h // G].max(0) + 1e-30
                 err = np.abs(out[t, h] - o)
                 assert (err <= tol).all(), (where, float((err - tol).max()), np.flatnonzero(~(err <= tol))[:4])
@@ -101,11 +102,7 @@ def test_attention_smallest_scales(gpu_lib, scale, q_lens, kv_lens, kind):
     log(f"attention scale {scale} {kind} {kv_lens}")
     out, lse = fq.fq_paged_attention(st.q, st.cache, st.batch, scale=scale, return_lse=True)
     torch.cuda.synchronize()
-    if kind == "bf16":
-        held = [[f64(t) for t in ts] for ts in (st.k, st.v)]
-        size = [[np.abs(t) for t in ts] for ts in held]
-    else:
-        held, size = held_codes(st)
+    held, size = rows_held([[f64(t) for t in ts] for ts in (st.k, st.v)]) if kind == "bf16" else held_codes(st)
     check_rows(out, lse, st.q, st.cu, held, size, q_lens, kv_lens, 128, float(np.float32(scale)), every=13)
 
 
@@ -168,3 +165,29 @@ def test_attention_infinities_of_no_weight(gpu_lib, at, tiles, kind):
         assert torch.equal(out[:, :, keep], clean[:, :, keep])
     else:
         assert torch.isnan(out[first:]).all()
+
+
+def rows_held(held):
+    """K and V of a bf16 step as check_rows takes them."""
+    return held, [[np.abs(t) for t in ts] for ts in held]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kind", ["bf16", "int8", "int4"])
+@pytest.mark.parametrize("name", list(STEPS) + ["many_" + n for n in MANY])
+def test_attention_within_the_magnitudes_of_its_summands(gpu_lib, name, kind, D):
+    """The steps of the other file with the tolerance that each kernel's own summands give: an
+    addition rounded to nearest (2^-24) of |q| s (c + z), with 4 bits of |q| s (16 + c + z),
+    and one rounding to bf16 (2^-8) of a weight and of the result."""
+    fq = gpu_lib
+    many = name.startswith("many_")
+    hq, hkv, page, q_lens, kv_lens, window, sinks = MANY[name[5:]] if many else STEPS[name]
+    st = Step(fq, kind, D, hq, hkv, page, q_lens, kv_lens, seed=5 * len(name) + D)
+    if many:
+        tiles_bounds(st, window, sinks, by_keys="split" in name and not window)
+    log(f"attention magnitudes {name} {kind} D={D}")
+    out, lse = fq.fq_paged_attention(st.q, st.cache, st.batch, window=window, sinks=sinks, return_lse=True)
+    torch.cuda.synchronize()
+    held, size = rows_held([[f64(t) for t in ts] for ts in (st.k, st.v)]) if kind == "bf16" else held_codes(st)
+    check_rows(out, lse, st.q, st.cu, held, size, q_lens, kv_lens, D, float(np.float32(D ** -0.5)), window, sinks,
+               every=11 if many else 3, unit=2.0 ** -24)
