@@ -191,3 +191,51 @@ def test_attention_within_the_magnitudes_of_its_summands(gpu_lib, name, kind, D)
     held, size = rows_held([[f64(t) for t in ts] for ts in (st.k, st.v)]) if kind == "bf16" else held_codes(st)
     check_rows(out, lse, st.q, st.cu, held, size, q_lens, kv_lens, D, float(np.float32(D ** -0.5)), window, sinks,
                every=11 if many else 3, unit=2.0 ** -24)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8", "int4"])
+@pytest.mark.parametrize("given", [True, False], ids=["stream_given", "stream_current"])
+def test_every_operator_runs_on_its_stream(gpu_lib, kind, given):
+    """All inputs of write, read, attention and norm are made on a side stream behind work that
+    keeps it busy, over contents that give other results: on any other stream the calls would
+    take those."""
+    fq = gpu_lib
+    st = Step(fq, kind, 128, 8, 2, 64, [1, 1], [4000, 77], seed=12)
+    slots = torch.cat([st.table[b].long()[t // 64] * 64 + t % 64 for b, t in ((0, torch.arange(4000)), (1, torch.arange(77)))])
+    names = ["q", "k", "v", "slots", "x", "res", "w"]
+    g = torch.Generator().manual_seed(9)
+    made = [st.q.clone(), torch.cat(st.k).cuda(), torch.cat(st.v).cuda(), slots.cuda(),
+            *(torch.randn(s, generator=g).to(torch.bfloat16).cuda() for s in ((64, 4096), (64, 4096), (4096,)))]
+    cache = fq.KVCache.empty(st.cache.n_pages, 64, 2, 128, kind)
+
+    def calls(t, stream):
+        fq.fq_kv_cache_write(cache, t["k"], t["v"], t["slots"], stream=stream)
+        k, v = fq.fq_kv_cache_read(cache, t["slots"], dtype="f32", stream=stream)
+        out, lse = fq.fq_paged_attention(t["q"], cache, st.batch, return_lse=True, stream=stream)
+        r, h = fq.fq_gated_residual_norm(t["x"], t["res"], t["w"], stream=stream)
+        return k, v, out, lse, r, h
+
+    want = [t.clone() for t in calls(dict(zip(names, made)), None)]
+    c = fq.fq_paged_attention_launch(8, 2, cache, st.batch)
+    assert c["split"] > 1
+    empty = {n: torch.full_like(t, -1) if n == "slots" else torch.zeros_like(t) for n, t in zip(names, made)}
+    busy = torch.randn((4096, 4096), device="cuda").to(torch.bfloat16)
+    for t in (cache.k, cache.v):
+        t.view(torch.uint8).zero_()
+    side, end = torch.cuda.Stream(), torch.cuda.Event()
+    log(f"operators on a side stream {kind} given={given}")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(400):
+            torch.mm(busy, busy)
+        for n, t in zip(names, made):
+            empty[n].copy_(t)
+        if not given:
+            got = calls(empty, None)
+    if given:
+        got = calls(empty, side)
+    end.record(side)
+    assert not end.query()   # the work before them was still under way when all had been enqueued
+    side.synchronize()
+    for n, a, b in zip(("k", "v", "out", "lse", "r", "h"), got, want):
+        assert torch.equal(a, b), n
