@@ -4,11 +4,7 @@
 
 #include <stdint.h>
 
-#ifdef __HIPCC__
-#define FQ_HOST_DEVICE __host__ __device__ __forceinline__
-#else
-#define FQ_HOST_DEVICE inline
-#endif
+#include "host_device.hpp"
 
 namespace fqi {
 

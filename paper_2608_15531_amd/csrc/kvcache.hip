@@ -15,8 +15,12 @@
 #include "device.hpp"
 #include "lanes.hpp"
 #include "layer.hpp"
+#include "quotient.hpp"
 
 namespace fqk {
+
+using fqi::inverse;
+using fqi::quotient;
 
 namespace {
 
@@ -66,14 +70,6 @@ __device__ __forceinline__ float bf16_up(float v) {
   return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, v) + 0xFFFFu) & 0xFFFF0000u);
 }
 
-// a / b correctly rounded from r = 1 / b correctly rounded: y = a r is next to it, a - y b
-// is exact, and one more step of it gives the rounded quotient (Markstein), far from the
-// ends of the range.  (Checked for b = 255 and 15 over all fp32, and for all bf16 a and b.)
-__device__ __forceinline__ float quotient(float a, float b, float r) {
-  const float y = a * r;
-  return fmaf(fmaf(-y, b, a), r, y);
-}
-
 // Quantises a row's 8 channels of this lane and stores them.  The scale is the smallest
 // bf16 not below span / top, and every quotient is the correctly rounded one: with
 // products by rounded inverses, spans that are a multiple of a bf16 would get the next
@@ -110,9 +106,7 @@ __device__ __forceinline__ void store_row(char* dst, uint32_t* meta, uint4 w, in
     uint32_t sb;
     if (span > 0x1p-90f && span < 0x1p90f) {
       s = bf16_up(quotient(span, top, 1.f / top));
-      // 1 / s: one step from an approximation within 2 of its last places is the rounded
-      // one for every s of 8 bits
-      const float r0 = __builtin_amdgcn_rcpf(s), r = fmaf(fmaf(-s, r0, 1.f), r0, r0);
+      const float r = inverse(s, __builtin_amdgcn_rcpf(s));
       zq = quotient(-lo, s, r);
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = quotient(x[j], s, r);
