@@ -538,8 +538,10 @@ fq_status fq_kv_cache_read(const fq_kv_cache* cache, const int64_t* slots, int64
  *   n_heads     query heads, a multiple of the cache's n_kv_heads: query head i reads KV
  *               head i / (n_heads / n_kv_heads).
  *   max_q,      upper bounds of the new tokens and of kv_lens over the sequences (>= 1);
- *   max_kv      up to 2^28; the kernel, its grid and (with total_q) the split of the keys
- *               follow from them, and the result only in its rounding.
+ *   max_kv      up to 2^28, and the blocks of 128 rows (token, query head) that max_q makes
+ *               in all below 2^24 (FQ_ERR_UNSUPPORTED); the kernel, its grid and (with
+ *               total_q) the split of the keys follow from them, and the result only in its
+ *               rounding.
  *               Tokens beyond max_q of a sequence are not computed and keys beyond
  *               max_kv are not seen.
  *   window      0: every token sees the keys up to its own.  W > 0: only the last W of

@@ -501,6 +501,8 @@ constexpr int64_t kTileBytes = int64_t(5) << 20;
 constexpr int64_t kEvenTiles = 160;
 // Partial results are bounded: 4096 ranges of 128 rows are 277 MB, 8192 of 16 rows 69.
 constexpr int64_t kMostTileRanges = 4096, kMostRanges = 8192;
+// Workgroups of 256 threads in one dimension of a grid: HIP takes fewer than 2^32 threads.
+constexpr int64_t kMostGrid = (int64_t(1) << 24) - 1;
 
 // Keys are numbered below 2^28, so a wider window sees the same ones; positions before the
 // first key less the window stay in 32 bits.
@@ -544,7 +546,9 @@ bool plan_attention(const fq_attention& a, const fq_kv_cache& c, AttnPlan* pl) {
     tiles = std::min<int64_t>(tiles, ceil_div(a.window + ceil_div(pl->rows, group), pl->tile) + 2 +
                                          ceil_div(a.sinks, pl->tile));
   int64_t split = 1;
-  if (items <= kMaxStrips) {   // every item has a counter
+  // every item has a counter, and the ranges and their join a grid
+  const int64_t most_split = kMostGrid / std::max<int64_t>(row_blocks * c.n_kv_heads, 1);
+  if (items <= kMaxStrips && most_split >= fqk::kJoinBlocks) {
     if (pl->kernel == FQ_ATTN_TILES) {
       const int64_t range_bytes = std::min<int64_t>(pl->rows, rows) * (c.head_dim + 4) * 4;
       const auto cost = [&](int64_t n) {
@@ -561,10 +565,11 @@ bool plan_attention(const fq_attention& a, const fq_kv_cache& c, AttnPlan* pl) {
           std::max(split, ceil_div(tiles, std::clamp<int64_t>(tiles / kEvenRanges, kEvenMinTiles, kEvenMaxTiles))),
           std::min<int64_t>(fqk::kMaxSplit, std::max<int64_t>(1, kMostRanges / items)));
     }
+    split = std::min(split, most_split);
   }
   pl->split_tiles = int(ceil_div(tiles, split));
   pl->split = int(ceil_div(tiles, pl->split_tiles));
-  if (pl->split * row_blocks * c.n_kv_heads > INT32_MAX) return false;
+  if (pl->split * row_blocks * c.n_kv_heads > kMostGrid) return false;
   pl->workgroups = grid * pl->split;
   if (pl->workgroups > INT32_MAX) return false;
   if (pl->kernel == FQ_ATTN_TILES) pl->lds_bytes = fqk::attn_tiles_lds(c.head_dim);

@@ -203,6 +203,9 @@ __device__ __forceinline__ void walk_partial_tiles(const AttnArgs& a, const Item
   }
 }
 
+// Workgroups of the join of a block of kTilesRows rows, with 128 channels.
+constexpr int kJoinBlocks = fqi::kTilesRows / 16;
+
 // attention_tiles.hip: the kernel for many rows, on `grid`.
 size_t attn_tiles_lds(int head_dim);
 int launch_attn_tiles(const AttnArgs& g, int kind, int head_dim, dim3 grid, hipStream_t s);

@@ -510,6 +510,7 @@ template <int D>
 __global__ void __launch_bounds__(256) join_kernel(AttnArgs a) {
   constexpr int T = D / 8, PER = 256 / T;   // threads a row, rows of a workgroup
   constexpr int kBlocks = kRows / PER;      // workgroups of a block of rows
+  static_assert(kBlocks <= kJoinBlocks, "the plan bounds the grid");
   Item it;
   const int x = int(blockIdx.x) / kBlocks, first = int(blockIdx.x) % kBlocks * PER;
   const int head = x % a.n_kv_heads, rb = x / a.n_kv_heads;

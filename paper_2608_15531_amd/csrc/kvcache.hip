@@ -12,6 +12,8 @@
 // TB/s.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "device.hpp"
 #include "lanes.hpp"
 #include "layer.hpp"
@@ -273,9 +275,21 @@ void by_kind(const fq_kv_cache& c, F&& f) {
   else with(std::integral_constant<int, FQ_KV_INT4>{});
 }
 
-dim3 token_grid(const fq_kv_cache& c, int64_t n_tokens) {
+dim3 token_grid(const fq_kv_cache& c, int n_tokens) {
   const int per = 256 / (c.head_dim / 8);
   return dim3(unsigned((n_tokens + per - 1) / per), unsigned(c.n_kv_heads));
+}
+
+// Tokens of one launch, of 16 threads and a head each at most: HIP takes fewer than 2^32
+// threads in one dimension of a grid.
+constexpr int64_t kMostTokens = int64_t(1) << 24;
+
+// f(first token, tokens) for each launch, while it returns 0.
+template <class F>
+int in_parts(int64_t n_tokens, F&& f) {
+  int e = 0;
+  for (int64_t t = 0; t < n_tokens && e == 0; t += kMostTokens) e = f(t, int(std::min(n_tokens - t, kMostTokens)));
+  return e;
 }
 
 }  // namespace
@@ -293,30 +307,36 @@ int launch_kv_write(const fq_kv_cache& c, const uint16_t* K, const uint16_t* V,
                     int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
                     int64_t v_head_stride, const int64_t* slots, int64_t n_tokens, void* stream) {
   const fqk::CacheArgs a = fqk::cache_args(c);
-  fqk::by_kind(c, [&](auto kind, auto dim) {
-    hipLaunchKernelGGL((fqk::kv_write_kernel<kind.value, dim.value>), fqk::token_grid(c, n_tokens), dim3(256), 0,
-                       static_cast<hipStream_t>(stream), a, K, V, k_token_stride, k_head_stride, v_token_stride,
-                       v_head_stride, slots, int(n_tokens));
+  return fqk::in_parts(n_tokens, [&](int64_t t, int n) {
+    fqk::by_kind(c, [&](auto kind, auto dim) {
+      hipLaunchKernelGGL((fqk::kv_write_kernel<kind.value, dim.value>), fqk::token_grid(c, n), dim3(256), 0,
+                         static_cast<hipStream_t>(stream), a, K + t * k_token_stride, V + t * v_token_stride,
+                         k_token_stride, k_head_stride, v_token_stride, v_head_stride, slots + t, n);
+    });
+    return int(hipGetLastError());
   });
-  return int(hipGetLastError());
 }
 
 int launch_kv_read(const fq_kv_cache& c, const int64_t* slots, int64_t n_tokens, void* K, void* V,
                    bool f32, void* stream) {
   const fqk::CacheArgs a = fqk::cache_args(c);
-  const bool past = 2 * n_tokens * c.n_kv_heads * c.head_dim * (f32 ? 4 : 2) > kStreamBytes;
-  fqk::by_kind(c, [&](auto kind, auto dim) {
-    auto go = [&](auto wide, auto streamed) {
-      hipLaunchKernelGGL((fqk::kv_read_kernel<kind.value, dim.value, wide.value, streamed.value>),
-                         fqk::token_grid(c, n_tokens), dim3(256), 0, static_cast<hipStream_t>(stream), a, slots,
-                         int(n_tokens), K, V);
-    };
-    if (f32 && past) go(std::true_type{}, std::true_type{});
-    else if (f32) go(std::true_type{}, std::false_type{});
-    else if (past) go(std::false_type{}, std::true_type{});
-    else go(std::false_type{}, std::false_type{});
+  const int64_t token_bytes = int64_t(c.n_kv_heads) * c.head_dim * (f32 ? 4 : 2);
+  const bool past = 2 * n_tokens * token_bytes > kStreamBytes;
+  return fqk::in_parts(n_tokens, [&](int64_t t, int n) {
+    fqk::by_kind(c, [&](auto kind, auto dim) {
+      auto go = [&](auto wide, auto streamed) {
+        hipLaunchKernelGGL((fqk::kv_read_kernel<kind.value, dim.value, wide.value, streamed.value>),
+                           fqk::token_grid(c, n), dim3(256), 0, static_cast<hipStream_t>(stream), a, slots + t, n,
+                           static_cast<void*>(static_cast<char*>(K) + t * token_bytes),
+                           static_cast<void*>(static_cast<char*>(V) + t * token_bytes));
+      };
+      if (f32 && past) go(std::true_type{}, std::true_type{});
+      else if (f32) go(std::true_type{}, std::false_type{});
+      else if (past) go(std::false_type{}, std::true_type{});
+      else go(std::false_type{}, std::false_type{});
+    });
+    return int(hipGetLastError());
   });
-  return int(hipGetLastError());
 }
 
 }  // namespace fqi

@@ -11,6 +11,8 @@
 // 4 rows of 4096: 3.2 us, a chain of loads, two sums over the workgroup and stores.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "device.hpp"
 #include "lanes.hpp"
 #include "layer.hpp"
@@ -197,8 +199,27 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormArgs a)
   }
 }
 
+// Rows of one launch, of up to 1024 threads each: HIP takes fewer than 2^32 threads in one
+// dimension of a grid.
+constexpr int kMostRows = 1 << 21;
+
+template <class T>
+T* from_row(T* p, int64_t row, int64_t stride) { return p ? p + row * stride : p; }
+
 template <class XT, class RT>
-int launch_typed(const NormArgs& a, hipStream_t s) {
+NormArgs part_of(const NormArgs& all, int64_t row) {
+  NormArgs a = all;
+  a.x = from_row(static_cast<const XT*>(all.x), row, all.x_stride);
+  a.residual = from_row(static_cast<const RT*>(all.residual), row, all.residual_stride);
+  a.gate = from_row(all.gate, row, all.gate_stride);
+  a.out = from_row(static_cast<RT*>(all.out), row, all.out_stride);
+  a.h = from_row(all.h, row, all.h_stride);
+  a.rows = int(std::min<int64_t>(all.rows - row, kMostRows));
+  return a;
+}
+
+template <class XT, class RT>
+int launch_part(const NormArgs& a, hipStream_t s) {
   const dim3 grid(a.rows), four((unsigned(a.rows) + 3) / 4);
   if (a.cols <= 512) hipLaunchKernelGGL((norm_kernel<XT, RT, 64, 1>), four, dim3(256), 0, s, a);
   else if (a.cols <= 1024) hipLaunchKernelGGL((norm_kernel<XT, RT, 64, 2>), four, dim3(256), 0, s, a);
@@ -208,6 +229,13 @@ int launch_typed(const NormArgs& a, hipStream_t s) {
   else if (a.cols <= 16384) hipLaunchKernelGGL((norm_kernel<XT, RT, 1024, 2>), grid, dim3(1024), 0, s, a);
   else hipLaunchKernelGGL((norm_kernel<XT, RT, 1024, 4>), grid, dim3(1024), 0, s, a);
   return int(hipGetLastError());
+}
+
+template <class XT, class RT>
+int launch_typed(const NormArgs& a, hipStream_t s) {
+  int e = 0;
+  for (int64_t row = 0; row < a.rows && e == 0; row += kMostRows) e = launch_part<XT, RT>(part_of<XT, RT>(a, row), s);
+  return e;
 }
 
 }  // namespace

@@ -239,3 +239,67 @@ def test_every_operator_runs_on_its_stream(gpu_lib, kind, given):
     side.synchronize()
     for n, a, b in zip(("k", "v", "out", "lse", "r", "h"), got, want):
         assert torch.equal(a, b), n
+
+
+def test_norm_of_more_rows_than_one_launch_takes(gpu_lib):
+    """2^26 rows of 64 threads are the 2^32 that no grid holds: rows at the ends of the launches
+    they are done in are those of calls of a few rows."""
+    fq = gpu_lib
+    M, H = (1 << 26) + 5, 4
+    log(f"norm {M} x {H}")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((M, H), generator=g, device="cuda", dtype=torch.bfloat16)
+    res = torch.randn((M, H), generator=g, device="cuda", dtype=torch.bfloat16)
+    gate = torch.rand((M, 8), generator=g, device="cuda").to(torch.bfloat16)[:, 2:6]
+    w = torch.ones(H, dtype=torch.bfloat16, device="cuda")
+    r, h = fq.fq_gated_residual_norm(x, res, w, post_weight=w, gate=gate)
+    for first in [0, *((p << 21) - 3 for p in (1, 2, 17, 31, 32))]:
+        at = slice(first, min(first + 8, M))
+        a, b = fq.fq_gated_residual_norm(x[at], res[at], w, post_weight=w, gate=gate[at])
+        torch.cuda.synchronize()
+        assert torch.equal(r[at], a) and torch.equal(h[at], b), first
+    assert torch.isfinite(h.view(-1)[::4097]).all() and (h != 0).any(1).all()
+
+
+def test_norm_of_wide_rows_over_launches(gpu_lib):
+    """fp32 and strided rows over the end of a launch."""
+    fq = gpu_lib
+    M, H = (1 << 21) + 7, 8
+    log(f"norm {M} x {H}")
+    wide = torch.randn((M, 24), device="cuda")
+    x, res = wide[:, 1:9], wide[:, 11:19]
+    w = torch.ones(H, dtype=torch.bfloat16, device="cuda")
+    r, h = fq.fq_gated_residual_norm(x, res, w, residual_scale=0.5)
+    at = slice(M - 12, M)
+    a, b = fq.fq_gated_residual_norm(x[at], res[at], w, residual_scale=0.5)
+    torch.cuda.synchronize()
+    assert torch.equal(r[at], a) and torch.equal(h[at], b)
+
+
+def test_cache_of_more_tokens_than_one_launch_takes(gpu_lib):
+    """2^29 tokens of 8 threads are the 2^32 that no grid holds; here nearly all of them are not
+    stored.  And a read over the end of a launch."""
+    fq = gpu_lib
+    n = (1 << 29) + 3
+    log(f"cache of {n} tokens")
+    cache = fq.KVCache.empty(2, 16, 1, 64, "int8")
+    row = torch.randn((1, 1, 64), device="cuda").to(torch.bfloat16)
+    slots = torch.full((n,), -1, dtype=torch.int64, device="cuda")
+    at = [0, (1 << 24) - 1, 1 << 24, (1 << 28) + 1, n - 1]
+    slots[at] = torch.arange(5, device="cuda") * 3
+    fq.fq_kv_cache_write(cache, row.expand(n, 1, 64), (-row).expand(n, 1, 64), slots)
+    del slots
+    k, v = fq.fq_kv_cache_read(cache, torch.arange(5, device="cuda") * 3, dtype="f32")
+    torch.cuda.synchronize()
+    for t, x in ((k, f64(row)), (v, -f64(row))):
+        want = L.held_rows(x, "int8").astype(np.float32)
+        assert (t.cpu().numpy() == want).all()
+    n = (1 << 24) + 9
+    slots = torch.arange(n, device="cuda") % 32
+    k, v = fq.fq_kv_cache_read(cache, slots)
+    part = fq.fq_kv_cache_read(cache, slots[(1 << 24) - 16:])
+    torch.cuda.synchronize()
+    stored = torch.isin(slots[(1 << 24) - 16:], torch.arange(5, device="cuda") * 3)
+    assert stored.any()
+    for t, p in ((k, part[0]), (v, part[1])):
+        assert torch.equal(t[(1 << 24) - 16:][stored], p[stored])

@@ -335,3 +335,32 @@ def test_numbers_below_32_bits_are_refused(name, value):
     with pytest.raises(ValueError):
         call(value)
     assert getattr(call(-1), name) == -1
+
+
+@pytest.mark.parametrize("heads", [(32, 8), (64, 64), (8, 1), (24, 1)])
+@pytest.mark.parametrize("total", [1, 5000, 1 << 22])
+def test_attention_grids_stay_within_hip_limits(lib, heads, total):
+    """Fewer than 2^32 threads in one dimension of a grid, of the kernel and of its join, for any
+    bounds; what cannot be launched so is refused."""
+    c = cache(n_kv_heads=heads[1], kind=fq.FQ_KV_BF16, n_pages=1 << 20)
+    launched = set()
+    for bits in range(8, 29, 2):
+        for max_kv in (100, 30000, 1 << 20):
+            for n_seqs in (1, 3, 100):
+                a = attn(n_seqs=n_seqs, n_heads=heads[0], max_q=1 << bits, max_kv=max_kv, total_q=total,
+                         table_cols=1 << 14)
+                out, n = (C.c_int32 * 8)(), C.c_size_t(0)
+                status = name(lib.fq_paged_attention_launch(C.byref(a), C.byref(c), out))
+                blocks = -(-(heads[0] // heads[1] << bits) // 128) * heads[1]
+                where = (bits, max_kv, n_seqs, list(out))
+                if blocks >= 1 << 24 or blocks * n_seqs >= 1 << 31:
+                    assert status == "FQ_ERR_UNSUPPORTED", where
+                    continue
+                assert status == "FQ_OK", where
+                launched.add(bits)
+                assert out[5] == out[2] * out[3] * heads[1] * n_seqs, where
+                assert out[5] // n_seqs * 256 < 1 << 32, where
+                if out[3] > 1 and out[0] == fq.FQ_ATTN_TILES:
+                    assert out[2] * heads[1] * 8 * 256 < 1 << 32, where
+                assert lib.fq_paged_attention_workspace_bytes(C.byref(a), C.byref(c), C.byref(n)) == 0
+    assert max(launched) >= 20
