@@ -856,6 +856,8 @@ def fq_kv_cache_read(cache: KVCache, slots, k=None, v=None, dtype="bf16", stream
     lib = load()
     index = cache._index
     f32 = dtype in ("f32", "fp32", torch.float32)
+    if not f32 and dtype not in ("bf16", "bfloat16", torch.bfloat16):
+        raise ValueError(f"dtype: bf16 or f32, got {dtype!r}")
     n = _check_slots(slots, index)
     shape = (n, cache.n_kv_heads, cache.head_dim)
     dt = torch.float32 if f32 else torch.bfloat16

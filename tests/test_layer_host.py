@@ -364,3 +364,12 @@ def test_attention_grids_stay_within_hip_limits(lib, heads, total):
                     assert out[2] * heads[1] * 8 * 256 < 1 << 32, where
                 assert lib.fq_paged_attention_workspace_bytes(C.byref(a), C.byref(c), C.byref(n)) == 0
     assert max(launched) >= 20
+
+
+@pytest.mark.parametrize("dtype", ["f16", "float16", "int8", None])
+def test_cache_read_refuses_other_types(lib, dtype):
+    from types import SimpleNamespace
+    torch = pytest.importorskip("torch")
+    c = SimpleNamespace(_index=-1, n_kv_heads=1, head_dim=64, device="cpu", _ref=None)
+    with pytest.raises(ValueError, match="dtype"):
+        fq.fq_kv_cache_read(c, torch.zeros(0, dtype=torch.int64), dtype=dtype)
