@@ -720,6 +720,13 @@ def _check_slots(slots, index):
     return n
 
 
+def _check_workspace(ws, index):
+    """A workspace of the caller; returns its bytes."""
+    if not isinstance(ws, _torch().Tensor) or ws.get_device() != index or not ws.is_contiguous():
+        raise ValueError(f"ws: expected a contiguous tensor on device {index}")
+    return ws.numel() * ws.element_size()
+
+
 def _any_stride(t):
     """Strides with 0 for dimensions of one, of which torch keeps any number."""
     return tuple(0 if n == 1 else s for n, s in zip(t.shape, t.stride()))
@@ -898,8 +905,8 @@ def fq_paged_attention(q, cache: KVCache, batch: PagedBatch, scale: float | None
     -infinity; rows of q that belong to no sequence are left as they are in `out`
     (unspecified in a new one).
 
-    ws: a zero-filled uint8 workspace of fq_paged_attention_workspace_bytes or more, for calls
-    that do not overlap in time.  Without one the workspace kept for the stream is used, which
+    ws: a zero-filled workspace of fq_paged_attention_workspace_bytes or more on the cache's
+    device, for calls that do not overlap in time.  Without one the workspace kept for the stream is used, which
     grows to the largest call's (277 MB of partial sums at most) and is not given back; a
     call recorded in a graph uses one in the graph's memory."""
     torch = _torch()
@@ -929,9 +936,9 @@ def fq_paged_attention(q, cache: KVCache, batch: PagedBatch, scale: float | None
     pl = None if lse is None else lse.data_ptr()
     capture = _capture_of(stream, sh) if ws is None else None
     w = _kept((index, sh), capture) if ws is None else ws
+    size = 0 if w is None else w.numel() if ws is None else _check_workspace(ws, index)
     status = lib.fq_paged_attention(ref, pq, cache._ref, cu, lens, table, po, pl,
-                                    None if w is None else w.data_ptr(),
-                                    0 if w is None else w.numel(), sh)
+                                    None if w is None else w.data_ptr(), size, sh)
     if status == _FQ_ERR_WORKSPACE and ws is None:
         # checked before anything is enqueued: none is kept yet, or too small a one
         need = C.c_size_t(0)

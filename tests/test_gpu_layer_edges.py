@@ -303,3 +303,18 @@ def test_cache_of_more_tokens_than_one_launch_takes(gpu_lib):
     assert stored.any()
     for t, p in ((k, part[0]), (v, part[1])):
         assert torch.equal(t[(1 << 24) - 16:][stored], p[stored])
+
+
+def test_workspaces_that_no_kernel_may_write_are_refused(gpu_lib):
+    """Before anything is launched; a workspace of any type counts by its bytes."""
+    fq = gpu_lib
+    st = Step(fq, "bf16", 128, 8, 2, 64, [1], [5000], seed=9)
+    need = fq.fq_paged_attention_workspace_bytes(8, 1, st.cache, st.batch)
+    log(f"workspaces of the caller, {need} bytes")
+    for bad in (torch.zeros(need, dtype=torch.uint8), torch.zeros(2 * need, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError, match="ws"):
+            fq.fq_paged_attention(st.q, st.cache, st.batch, ws=bad)
+    with pytest.raises(fq.FqError):
+        fq.fq_paged_attention(st.q, st.cache, st.batch, ws=torch.zeros(need - 4, dtype=torch.uint8, device="cuda"))
+    ws = torch.zeros(-(-need // 4), dtype=torch.int32, device="cuda")
+    assert torch.equal(fq.fq_paged_attention(st.q, st.cache, st.batch, ws=ws), fq.fq_paged_attention(st.q, st.cache, st.batch))

@@ -373,3 +373,15 @@ def test_cache_read_refuses_other_types(lib, dtype):
     c = SimpleNamespace(_index=-1, n_kv_heads=1, head_dim=64, device="cpu", _ref=None)
     with pytest.raises(ValueError, match="dtype"):
         fq.fq_kv_cache_read(c, torch.zeros(0, dtype=torch.int64), dtype=dtype)
+
+
+def test_workspaces_of_the_caller_are_checked():
+    """One in host memory, on another device or with gaps would be written where it is not."""
+    torch = pytest.importorskip("torch")
+    t = torch.zeros(64, dtype=torch.int32)
+    assert fq._check_workspace(t, -1) == 256   # -1: host memory, as the device asked for
+    for bad in (t[::2], None, 5):
+        with pytest.raises(ValueError, match="ws"):
+            fq._check_workspace(bad, -1)
+    with pytest.raises(ValueError, match="ws"):
+        fq._check_workspace(t, 0)
