@@ -414,11 +414,23 @@ def _stream_handle(stream, device) -> int:
 _raw_stream = None
 
 
+def _current_device() -> int:
+    return _torch()._C._cuda_getDevice()   # as torch.cuda.current_device, once a tensor is there
+
+
+def _elsewhere(index: int) -> bool:
+    """Whether device `index` is not the current one.  Its default stream has the handle of
+    every device's, and the library would launch on the current device's."""
+    return _current_device() != index
+
+
 def _stream_of(stream, index: int) -> int:
     """_stream_handle by device index, without making a torch Stream object of the current
     stream (1.5 us a call) where torch offers its handle."""
     global _raw_stream
     if stream is not None:
+        if stream.device_index != index:
+            raise ValueError(f"the stream is on device {stream.device_index}, the tensors on {index}")
         return int(stream.cuda_stream)
     if _raw_stream is None:
         torch = _torch()
@@ -846,6 +858,9 @@ def fq_kv_cache_write(cache: KVCache, k, v, slots, stream=None) -> None:
     out of range, such as -1, is not stored), quantised as the cache's kind asks."""
     lib = load()
     index, bf16 = cache._index, _torch().bfloat16
+    if _elsewhere(index):
+        with _torch().cuda.device(index):
+            return fq_kv_cache_write(cache, k, v, slots, stream)
     n = _check_slots(slots, index)
     shape = (n, cache.n_kv_heads, cache.head_dim)
     ks = _rows(k, bf16, shape, "k", index)
@@ -865,6 +880,9 @@ def fq_kv_cache_read(cache: KVCache, slots, k=None, v=None, dtype="bf16", stream
     f32 = dtype in ("f32", "fp32", torch.float32)
     if not f32 and dtype not in ("bf16", "bfloat16", torch.bfloat16):
         raise ValueError(f"dtype: bf16 or f32, got {dtype!r}")
+    if _elsewhere(index):
+        with torch.cuda.device(index):
+            return fq_kv_cache_read(cache, slots, k, v, dtype, stream)
     n = _check_slots(slots, index)
     shape = (n, cache.n_kv_heads, cache.head_dim)
     dt = torch.float32 if f32 else torch.bfloat16
@@ -914,6 +932,9 @@ def fq_paged_attention(q, cache: KVCache, batch: PagedBatch, scale: float | None
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q: expected [total_q][n_heads][head_dim]")
     index, bf16 = cache._index, torch.bfloat16
+    if _elsewhere(index):
+        with torch.cuda.device(index):
+            return fq_paged_attention(q, cache, batch, scale, window, sinks, out, return_lse, stream, ws)
     total, heads, _ = q.shape
     shape = (total, heads, cache.head_dim)
     qs = _rows(q, bf16, shape, "q", index)
@@ -1000,6 +1021,10 @@ def fq_gated_residual_norm(x, residual=None, pre_weight=None, post_weight=None, 
     if not x.is_cuda:   # below, the others are only compared with its device
         raise TypeError("x must be a CUDA (HIP) tensor")
     index, bf16, shape, xt = x.get_device(), torch.bfloat16, x.shape, x.dtype
+    if _elsewhere(index):
+        with torch.cuda.device(index):
+            return fq_gated_residual_norm(x, residual, pre_weight, post_weight, gate, residual_scale, eps,
+                                          residual_out, h, stream)
     M, H = shape
     xs = _rows(x, xt, shape, "x", index)
     rt, rs, gs, pr, pg = xt, 0, 0, None, None

@@ -385,3 +385,43 @@ def test_workspaces_of_the_caller_are_checked():
             fq._check_workspace(bad, -1)
     with pytest.raises(ValueError, match="ws"):
         fq._check_workspace(t, 0)
+
+
+@pytest.mark.parametrize("call", ["write", "read", "attention"])
+def test_calls_make_the_tensors_device_current(lib, monkeypatch, call):
+    """With another device current its default stream, which has the same handle, would run the
+    kernel.  (The calls then stop at their first tensor check: there is no GPU here.)"""
+    from types import SimpleNamespace
+    torch = pytest.importorskip("torch")
+    current, seen = [0], []
+
+    class device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            self.before, current[0] = current[0], self.index
+            seen.append(self.index)
+
+        def __exit__(self, *exc):
+            current[0] = self.before
+
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(fq, "_current_device", lambda: current[0])
+    c = SimpleNamespace(_index=1, n_kv_heads=1, head_dim=64, device="cuda:1", _ref=None)
+    t = torch.zeros((1, 1, 64), dtype=torch.bfloat16)
+    with pytest.raises((TypeError, ValueError)):
+        if call == "write":
+            fq.fq_kv_cache_write(c, t, t, None)
+        elif call == "read":
+            fq.fq_kv_cache_read(c, None)
+        else:
+            fq.fq_paged_attention(t, c, SimpleNamespace(_index=1))
+    assert seen == [1] and current == [0]
+
+
+def test_streams_of_other_devices_are_refused():
+    from types import SimpleNamespace
+    with pytest.raises(ValueError, match="stream"):
+        fq._stream_of(SimpleNamespace(device_index=1, cuda_stream=5), 0)
+    assert fq._stream_of(SimpleNamespace(device_index=1, cuda_stream=5), 1) == 5
