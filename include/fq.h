@@ -16,7 +16,8 @@
  * Conventions used by every entry point:
  *   - All functions return an fq_status; no C++ exception crosses the ABI.
  *   - Sizes and strides are in elements unless stated otherwise; the stride of a
- *     dimension of size one is ignored.
+ *     dimension of size one is ignored.  Inputs may repeat rows (strides of 0); rows of
+ *     outputs do not overlap (FQ_ERR_SHAPE where a stride is shorter than a row).
  *   - Every argument check runs on the host before anything is launched;
  *     a failed check launches nothing and leaves every output untouched.
  *   - Device entry points only enqueue work on the caller's HIP stream and

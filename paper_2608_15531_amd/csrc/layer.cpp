@@ -19,6 +19,20 @@ bool is_stride(int64_t s, int64_t unit) { return s >= 0 && s % unit == 0; }
 // keep any number there.
 int64_t used(int64_t stride, int64_t n) { return n > 1 ? stride : 0; }
 
+// Rows of `row` units, n of them `stride` apart, lie over one another: different workgroups
+// would write the same memory.
+bool overlap(int64_t stride, int64_t n, int64_t row) { return n > 1 && stride < row; }
+
+// The same of a cache's rows and words that are to be written.
+bool overlap(const fq_kv_cache& c) {
+  const int64_t row = c.kind == FQ_KV_BF16 ? 2 * c.head_dim : c.kind == FQ_KV_INT8 ? c.head_dim : c.head_dim / 2;
+  if (overlap(c.page_stride, c.n_pages, row) || overlap(c.head_stride, c.n_kv_heads, row) ||
+      overlap(c.token_stride, c.page_size, row))
+    return true;
+  return c.kind != FQ_KV_BF16 && (overlap(c.meta_page_stride, c.n_pages, c.page_size) ||
+                                  overlap(c.meta_head_stride, c.n_kv_heads, c.page_size));
+}
+
 // Sizes, kind and strides: all that needs no pointer.
 fq_status check_cache_sizes(const fq_kv_cache* c) {
   if (!c) return FQ_ERR_NULL;
@@ -87,7 +101,7 @@ fq_status fq_kv_cache_write(const fq_kv_cache* cache, const uint16_t* K, const u
                             int64_t n_tokens, void* stream) {
   const fq_status st = check_cache(cache);
   if (st != FQ_OK) return st;
-  if (n_tokens < 0) return FQ_ERR_SHAPE;
+  if (n_tokens < 0 || overlap(*cache)) return FQ_ERR_SHAPE;
   k_token_stride = used(k_token_stride, n_tokens);
   v_token_stride = used(v_token_stride, n_tokens);
   k_head_stride = used(k_head_stride, cache->n_kv_heads);
@@ -152,6 +166,8 @@ fq_status fq_paged_attention(const fq_attention* a, const uint16_t* Q, const fq_
   fq_status st = check_attention(a, cache);
   if (st == FQ_OK) st = check_cache(cache);
   if (st != FQ_OK) return st;
+  if (overlap(a->o_token_stride, a->total_q, cache->head_dim) || overlap(a->o_head_stride, a->n_heads, cache->head_dim))
+    return FQ_ERR_SHAPE;
   if (a->total_q == 0) return FQ_OK;
   if (!Q || !cu_q || !kv_lens || !block_table || !O) return FQ_ERR_NULL;
   if (!aligned(Q, 16) || !aligned(O, 16) || !aligned(lse, 4) || !aligned(cu_q, 4) ||
@@ -178,6 +194,8 @@ fq_status fq_gated_residual_norm(const fq_norm* n, const void* x, const void* re
       (n->residual_dtype != FQ_Y_BF16 && n->residual_dtype != FQ_Y_F32) || n->cols > 32768 ||
       n->rows > INT32_MAX)
     return FQ_ERR_UNSUPPORTED;
+  if ((residual_out && overlap(n->residual_out_stride, n->rows, n->cols)) || (h && overlap(n->h_stride, n->rows, n->cols)))
+    return FQ_ERR_SHAPE;
   if (n->rows == 0) return FQ_OK;
   if (!residual_out && !h) return FQ_ERR_NULL;
   if (!x || (h && !pre_weight)) return FQ_ERR_NULL;

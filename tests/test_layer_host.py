@@ -425,3 +425,38 @@ def test_streams_of_other_devices_are_refused():
     with pytest.raises(ValueError, match="stream"):
         fq._stream_of(SimpleNamespace(device_index=1, cuda_stream=5), 0)
     assert fq._stream_of(SimpleNamespace(device_index=1, cuda_stream=5), 1) == 5
+
+
+def test_overlapping_outputs_are_refused(lib):
+    """Rows over one another would be written by several workgroups; inputs may repeat rows."""
+    def write(**kw):
+        return name(lib.fq_kv_cache_write(C.byref(cache(**kw)), FAKE, FAKE, 0, 0, 0, 0, FAKE, 0, None))
+
+    assert write() == "FQ_OK"
+    for kw in (dict(head_stride=0), dict(token_stride=0), dict(page_stride=64), dict(meta_head_stride=32),
+               dict(meta_page_stride=0), dict(kind=fq.FQ_KV_BF16, token_stride=128)):
+        assert write(**kw) == "FQ_ERR_SHAPE", kw
+    assert write(n_pages=1, page_stride=0, meta_page_stride=0) == "FQ_OK"
+    assert write(kind=fq.FQ_KV_BF16, meta_page_stride=0, meta_head_stride=0) == "FQ_OK"
+
+    c = cache()
+
+    def attend(**kw):
+        a = attn(**kw)
+        return name(lib.fq_paged_attention(C.byref(a), FAKE, C.byref(c), FAKE, FAKE, FAKE, None, None, FAKE, 1 << 40, None))
+
+    assert attend() == "FQ_ERR_NULL"   # O: checked after the strides
+    assert attend(q_token_stride=0, q_head_stride=0) == "FQ_ERR_NULL"
+    for kw in (dict(o_token_stride=0), dict(o_head_stride=64), dict(o_head_stride=0)):
+        assert attend(**kw) == "FQ_ERR_SHAPE", kw
+    assert attend(total_q=1, o_token_stride=0) == "FQ_ERR_NULL"
+
+    def norm(out=FAKE, h=FAKE, **kw):
+        d = dict(rows=4, cols=128, x_dtype=0, residual_dtype=0, eps=1e-5, residual_scale=1.0, x_stride=0,
+                 residual_stride=0, gate_stride=0, residual_out_stride=128, h_stride=128)
+        d.update(kw)
+        return name(lib.fq_gated_residual_norm(C.byref(fq.fq_norm(**d)), None, FAKE, None, None, FAKE, out, h, None))
+
+    assert norm() == "FQ_ERR_NULL"     # x: checked after the strides
+    assert norm(residual_out_stride=0) == norm(h_stride=127) == "FQ_ERR_SHAPE"
+    assert norm(out=None, residual_out_stride=0) == norm(rows=1, h_stride=0) == "FQ_ERR_NULL"
