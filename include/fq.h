@@ -580,7 +580,8 @@ typedef struct {
 /*
  * fq_paged_attention_workspace_bytes -- the workspace of fq_paged_attention: the
  * same kind of workspace as the matmuls' (fq_workspace_bytes: counters that are zero
- * between calls, then scratch), so that one buffer may serve both in turn.
+ * between calls, then scratch), so that one buffer may serve both in turn.  The scratch holds
+ * the partial sums of the ranges, 277 MB at most (FQ_ATTN_TILES).
  */
 fq_status fq_paged_attention_workspace_bytes(const fq_attention* a, const fq_kv_cache* cache,
                                              size_t* bytes);
@@ -608,7 +609,9 @@ fq_status fq_paged_attention_launch(const fq_attention* a, const fq_kv_cache* ca
  *   lse          device fp32 [total_q][n_heads]: ln of the sum of exp(scale q.k); NULL: not
  *                written.
  * Q, O 16-byte aligned.  Scores, softmax statistics and sums are held in fp32; the softmax
- * weights (times the scale of V's row) are rounded to bf16 as the matrix operand.  The sums of the
+ * weights (times the scale of V's row) are rounded to bf16 as the matrix operand.  A weight is
+ * up to 2^8 before the division by their sum, so with |V| below 2^116 / max_kv no sum passes
+ * fp32; larger ones may give infinities or NaN.  The sums of the
  * ranges are added in their order, so equal calls give equal bits.  Index contents out of
  * range cannot make the kernel read or write out of bounds but give unspecified values.
  * Rows of O that belong to no sequence are not written.

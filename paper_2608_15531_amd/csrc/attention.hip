@@ -24,8 +24,11 @@
 // The offset's own sums cancel in fp32: with 128 + c, a bf16's last bits, the log-sum over
 // three keys was off by 5e-7 of itself, with 16 + c by what it is off in bf16.
 //
-// Memory bounds it: 64 sequences of 100 to 8190 keys at 8 bits take 129 us, 4.3 TB/s, and
-// 16 of 24000 to 32767 at 4 bits, 64 heads, 101 us, 4.9 TB/s (a copy: 4.9).  One token over
+// The weights (times s_v) of the second product are bf16, as its operand: in fp32 each would
+// take two.  They move a row by up to 2^-8 sum w |v|; statistics and sums are fp32.
+//
+// Memory bounds it: 64 sequences of 100 to 8190 keys at 8 bits take 130 us, 4.3 TB/s, and
+// 16 of 24000 to 32767 at 4 bits, 64 heads, 101 us, 4.9 TB/s (a copy: 5.1).  One token over
 // 1000 keys takes 8 us, which is latency.  16 rows and no LDS keep four waves a SIMD under
 // way; loads for the next tile in further registers cost a third of them, and 107 became
 // 120 us for the 16 sequences.
@@ -478,26 +481,27 @@ constexpr int kEvenRanges = 8, kEvenMinTiles = 24, kEvenMaxTiles = 128;
 // The kernel for few rows reads the keys once for each block of 16 rows, the one for many
 // once for 128, at a longer start and with a second kernel for the join.  By measurement
 // (us, few / many), with what the blocks of 16 rows read in all: 40 tokens of 4 heads a
-// group over 540 keys, bf16, 22 MB: 10 / 18; 16 over 8000, bf16, 131 MB: 23 / 31; 300 over
-// 600, bf16, 184 MB: 18 / 27; 10 over 2000, 16 sequences, 8 bits, 204 MB: 31 / 40; but 16
-// over 4000, 8 sequences, 8 bits, 271 MB: 44 / 41; 20 over 2000, 8 sequences, bf16, 331 MB:
-// 34 / 28.
+// group over 540 keys, bf16, 22 MB: 10 / 18; 16 over 8000, bf16, 131 MB: 25 / 23; 300 over
+// 600, bf16, 184 MB: 19 / 27; 10 over 2000, 16 sequences, 8 bits, 204 MB: 38 / 44; 16 over
+// 4000, 8 sequences, 8 bits, 271 MB: 46 / 46; 20 over 2000, 8 sequences, bf16, 331 MB: 35 / 27.
 constexpr int64_t kFewRowsBytes = int64_t(224) << 20;
 // The kernel for many rows has two workgroups to a CU; it splits the keys where that makes
 // rounds * (tiles of a range + kRangeCost) + bytes of the partial sums / kTileBytes smaller:
 // a range's start and its part in the join are worth so many tiles, and in a tile's time, 2.3
 // us, that many bytes are written and read again.
 // (Up to 2048 ranges: with more of them, not all of the longest sequence's length, the rounds
-// say little; 20 to 900 tokens of 8 sequences over 500 to 8000 keys went from 546 to 678 us.)
+// say little.  With 4096 20 to 900 tokens of 8 sequences over 500 to 8000 keys went from 534 to
+// 673 us, but 2000, 10 and 100 over 0, 8000 and 20000, 4 bits, 64 heads, from 693 to 508.)
 constexpr int kTileSlots = 512;
 constexpr int kRangeCost = 4;
 constexpr int kRoundsRanges = 2048;
 constexpr int64_t kTileBytes = int64_t(5) << 20;
 // Of several sequences one may be much longer than the others, and its ranges then are what
-// takes long: they have 10240 keys at most.  (us, without / with: 5 to 300 tokens of 6
-// sequences over 500 to 30000 keys, 8 bits: 1126 / 655; 2000, 10 and 100 over 0, 8000 and
-// 20000, 4 bits, 64 heads: 969 / 710; but 4 times 1024 over 16000, 8 bits: 1549 / 1583.  With
-// 4096 keys 20 to 900 tokens of 8 sequences over 500 to 8000 went from 603 to 633.)
+// takes long: they have 10240 keys at most.  (us, without / with: 2000, 10 and 100 tokens over
+// 0, 8000 and 20000 keys, 4 bits, 64 heads: 979 / 693; 5 to 300 of 6 sequences over 500 to
+// 30000, 8 bits: 693 both; but equal ones are split too, 4 times 1024 over 16000, 8 bits: 1579
+// / 1637.  With 4096 keys the first took 509, but 20 to 900 tokens of 8 sequences over 500 to
+// 8000 564 instead of 534, and the second 764.)
 constexpr int64_t kEvenTiles = 160;
 // Partial results are bounded: 4096 ranges of 128 rows are 277 MB, 8192 of 16 rows 69.
 constexpr int64_t kMostTileRanges = 4096, kMostRanges = 8192;

@@ -21,11 +21,18 @@
 // fp32 number (700 tokens over 2700 keys, 8 bits: 92 us; as 32 multiply-adds 95; 88 with
 // c - z formed in LDS, which holds whole z up to 255 only).
 //
-// 2048 tokens over 8192 keys, 32 heads on 8, D = 128, bf16: 263 to 293 us, 820 to 915
-// TFLOP/s (a product of 8192^3: 1213).  The matrix cores are busy 39 % of the time:
-// a wave's tile takes about 200 vector instructions beside 32 products, and 256 registers
-// leave no room to compute one tile's scores beside another's softmax (374 us, with
-// spills); two workgroups to a CU overlap each other.  256 rows a workgroup: 300 us.
+// The weights of the second product are bf16, as its operand (in fp32 each would take two and
+// the product twice as long); they are what a row's error is beyond its own rounding, up to
+// 2^-8 sum w |v|.  Statistics and sums are fp32.
+//
+// 2048 tokens over 8192 keys, 32 heads on 8, D = 128, bf16: 264 to 274 us, 880 to 912
+// TFLOP/s (a product of 8192^3, both operands along k: 1630).  The matrix cores are busy 39 %
+// of the time: a wave's tile takes 32 products, about 1000 cycles, and about 200 vector
+// instructions, 32 of them exponentials at a quarter of the rate, about 1200 more, and by
+// these numbers the one hardly runs beside the other.  One barrier a tile keeps the waves of
+// a workgroup in the same phase, nothing holds the two workgroups of a CU in opposite ones,
+// and 256 registers leave no room to compute one tile's scores beside another's softmax
+// (374 us, with spills).  256 rows a workgroup: 300 us.
 #include "attention.hpp"
 
 namespace fqk {

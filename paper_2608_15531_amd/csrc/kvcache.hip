@@ -5,7 +5,7 @@
 // of a token and head, both loads first.  A workgroup takes consecutive tokens of one head:
 // in a page these rows follow one another, so their stores fill whole cache lines.
 //
-// Memory bounds both kernels (a copy of 2 GiB: 4.9 TB/s), and with codes the arithmetic of
+// Memory bounds both kernels (a copy of 1 GiB: 5.1 TB/s), and with codes the arithmetic of
 // the write stands next to it.  4096 tokens of 8 heads x 128, bf16, written: 5.8 us, 5.8
 // TB/s; 12001 tokens at 4 bits: written in 13.7 us, 4.5 TB/s (18 with general divisions and
 // conversions), read back in 12, 5.2 TB/s; 30007 tokens at 8 bits read as fp32: 49 us, 6.3

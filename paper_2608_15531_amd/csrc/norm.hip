@@ -7,7 +7,7 @@
 // A row stays in the registers of the threads that share it (8 columns a thread at a
 // time) from its one read to its one write, so both means cost no second pass.  The
 // kernel is bound by memory: 13 operations against 10 bytes and more an element.  8191
-// rows of 8192, bf16 x and gate, fp32 residual: 196 us, 4.8 TB/s (a copy of 2 GiB: 4.9);
+// rows of 8192, bf16 x and gate, fp32 residual: 196 us, 4.8 TB/s (a copy of 1 GiB: 5.1);
 // 4 rows of 4096: 3.2 us, a chain of loads, two sums over the workgroup and stores.
 #include <hip/hip_runtime.h>
 
